@@ -421,6 +421,121 @@ pic_status pic_decode_attn_noalloc(const pic_model* model, const void* q, const 
                                    int32_t max_base_len, float scale, int32_t n_splits, void* out,
                                    void* stream);
 
+/* ---- 5. paged cache: a cache handed out in pages (App. C.1's token map from slots to rows, page by page) ----
+   A paged cache holds K and V as two buffers in the pool's layout,
+       pages  [L][Hkv][n_pages * page_tokens][D]
+   page p being rows [p * page_tokens, (p + 1) * page_tokens) of every (layer, kv head), and a
+   page table [batch][table_cap] of page numbers: slot t (logical position) of request b lives in
+   row table[b][t / page_tokens] * page_tokens + t % page_tokens.  Requests may share pages (a composed
+   context sampled several times); a page that a call writes must belong to one request only.
+   The buffers are also a cache of batch 1 and cache_cap n_pages * page_tokens: pic_compose and
+   pic_compose_shared fill pages from documents through the blocks that pic_page_blocks gives.
+     n_pages      pages per buffer; n_pages * page_tokens at most INT32_MAX
+     page_tokens  a power of two from 16 to 1024
+     table_cap    entries per request in the page table
+   Table entries are read as given: one outside [0, n_pages) reads some other page's rows (entry
+   clamped) and stores nothing.  Only entries of pages that hold a visible slot matter. */
+typedef struct {
+  int32_t n_pages;
+  int32_t page_tokens;
+  int32_t table_cap;
+} pic_pages;
+
+/* ---- 5a. page bookkeeping (host only) ----
+   The caller holds the page table on the host ([batch][table_cap], -1: no page) and a reference
+   count per page (refs [n_pages], 0: free; zeroed to begin with); these calls keep the two in step.
+   A call that fails changes neither.  Entries that are neither -1 nor a page with a reference fail
+   with PIC_ERR_RANGE where the call meets them.
+
+   pic_page_grow makes requests ready to store slots [len[b], new_len[b]): it gives each the pages it
+   lacks, lowest free page first, and where the page that holds slot len[b] is partly filled and
+   shared, a page of its own with a (source, destination) pair in `pairs` for pic_page_copy.  Requests
+   with new_len[b] <= len[b] are left alone.
+     pairs [host out, pair_cap x 2]   room for batch pairs is always enough
+     n_pairs [host out]               pairs written
+   PIC_ERR_CAPACITY when the free pages, pair_cap or table_cap do not suffice.
+   pic_page_fork lets request dst (which must hold no page: PIC_ERR_INVALID_ARG) share the pages of
+   request src that hold slots [0, len).
+   pic_page_free lets go of a request's pages past its first keep_len slots (0: all of them).
+   pic_page_compact renumbers the pages in use to [0, n_used), rewriting refs and the table, and
+   names the moves in `pairs` (sources and destinations never overlap).  Every reference must be in
+   this table (PIC_ERR_INVALID_ARG otherwise); PIC_ERR_CAPACITY when pair_cap (n_pages / 2 is always
+   enough) does not suffice, with *n_pairs the pairs needed.
+   pic_page_blocks rewrites gather blocks (pic_plan_layout / pic_plan_frontier) into blocks of the
+   paged buffers, cut where pages end: request 0, dst_slot the row of the page.  PIC_ERR_RANGE for a
+   block outside the table or over an entry that is no page, PIC_ERR_CAPACITY with *n_out the blocks
+   needed when out_cap is too small. */
+pic_status pic_page_grow(const pic_pages* pages, int32_t batch, int32_t* refs, int32_t* page_table,
+                         const int32_t* len, const int32_t* new_len, int32_t* pairs, int32_t pair_cap,
+                         int32_t* n_pairs);
+pic_status pic_page_fork(const pic_pages* pages, int32_t batch, int32_t* refs, int32_t* page_table,
+                         int32_t src, int32_t len, int32_t dst);
+pic_status pic_page_free(const pic_pages* pages, int32_t batch, int32_t* refs, int32_t* page_table,
+                         int32_t request, int32_t keep_len);
+pic_status pic_page_compact(const pic_pages* pages, int32_t batch, int32_t* refs, int32_t* page_table,
+                            int32_t* pairs, int32_t pair_cap, int32_t* n_pairs, int32_t* n_used);
+pic_status pic_page_blocks(const pic_pages* pages, int32_t batch, const int32_t* page_table,
+                           const pic_block* blocks, int32_t n_blocks, pic_block* out, int32_t out_cap,
+                           int32_t* n_out);
+
+/* ---- 5b. page copies ----
+   Page pairs[i][1] = page pairs[i][0], whole, in every layer and kv head of both buffers: what a
+   shared page's first write (pic_page_grow) and a compaction ask for.
+     pairs [host, n_pairs x 2]   read before the call returns.  All copies are as if at once: a page
+                                 that is written twice, or both read and written, fails with
+                                 PIC_ERR_INVALID_ARG, one outside [0, n_pages) with PIC_ERR_RANGE
+   table_cap is ignored. */
+pic_status pic_page_copy(const pic_model* model, const pic_pages* pages, void* pages_k, void* pages_v,
+                         const int32_t* pairs, int32_t n_pairs, void* stream);
+
+/* ---- 5c. suffix prefill over pages ----
+   pic_suffix_prefill_attn on a paged cache: stores k_suf / v_suf of token i < n_valid[b] of request
+   b at slot ctx_len[b] + i and computes its attention over slots [0, ctx_len[b] + i].  Outputs are
+   bit-identical to pic_suffix_prefill_attn's on the same cache contents with the same workspace, where
+   every token is valid.
+     page_table [device, batch x table_cap]
+     ctx_len    [device, batch]   clamped to max_ctx; a negative one marks a request that is only
+                                  padding: nothing of it is read, stored or computed
+     n_valid    [device, batch]   tokens used per request, clamped to [0, n_suffix]; the others are neither
+                                  stored nor computed, their out rows left untouched.  NULL: all
+     max_ctx + n_suffix <= table_cap * page_tokens (PIC_ERR_CAPACITY)
+     (q, k_suf, v_suf, out, scale and the workspace as for pic_suffix_prefill_attn; bf16 pages:
+     n_pages * page_tokens and n_suffix * Hkv below 2^24)
+   pic_page_suffix_attn_rope: q and k_suf unrotated, as for pic_suffix_prefill_attn_rope.  bf16 only. */
+pic_status pic_page_suffix_attn(const pic_model* model, const pic_pages* pages, const void* q,
+                                const void* k_suf, const void* v_suf, void* pages_k, void* pages_v,
+                                const int32_t* page_table, int32_t batch, const int32_t* ctx_len,
+                                int32_t max_ctx, const int32_t* n_valid, int32_t n_suffix, float scale,
+                                void* out, void* workspace, size_t ws_bytes, void* stream);
+pic_status pic_page_suffix_attn_rope(const pic_model* model, const pic_pages* pages, const void* q,
+                                     const void* k_suf, const void* v_suf, void* pages_k, void* pages_v,
+                                     const int32_t* page_table, int32_t batch, const int32_t* ctx_len,
+                                     int32_t max_ctx, const int32_t* n_valid, int32_t n_suffix,
+                                     const void* table, int32_t max_abs_delta, float scale, void* out,
+                                     void* workspace, size_t ws_bytes, void* stream);
+
+/* ---- 5d. decode over pages ----
+   pic_decode_attn on a paged cache: stores the new token at slot p = base_len[b] + step and attends
+   over slots [0, p]; split over the context and joined alike.  Outputs are bit-identical to
+   pic_decode_attn's on the same cache contents and lengths for the same n_splits and workspace.
+     page_table [device, batch x table_cap]
+     base_len   [device, batch]   clamped to max_base_len; a negative one marks padding of the batch:
+                                  nothing of that request is read or stored, its out rows are left untouched
+     max_base_len + step + 1 <= table_cap * page_tokens (PIC_ERR_CAPACITY)
+     (the other arguments and the workspace as for pic_decode_attn)
+   pic_page_decode_attn_rope: q and k_new unrotated, as for pic_decode_attn_rope.  bf16 only. */
+pic_status pic_page_decode_attn(const pic_model* model, const pic_pages* pages, const void* q,
+                                const void* k_new, const void* v_new, void* pages_k, void* pages_v,
+                                const int32_t* page_table, int32_t batch, const int32_t* base_len,
+                                int32_t step, int32_t max_base_len, float scale, int32_t n_splits,
+                                void* out, void* workspace, size_t ws_bytes, void* stream);
+pic_status pic_page_decode_attn_rope(const pic_model* model, const pic_pages* pages, const void* q,
+                                     const void* k_new, const void* v_new, void* pages_k, void* pages_v,
+                                     const int32_t* page_table, int32_t batch, const int32_t* base_len,
+                                     int32_t step, int32_t max_base_len, const void* table,
+                                     int32_t max_abs_delta, float scale, int32_t n_splits, void* out,
+                                     void* workspace, size_t ws_bytes, void* stream);
+
 /* ---- diagnostics ---- */
 const char* pic_status_string(pic_status status);
 /* Thread-local description of the last failure on this thread ("" if none). */

@@ -31,7 +31,9 @@ EXPORTS = ("pic_plan_layout", "pic_plan_frontier", "pic_rope_table_bytes", "pic_
            "pic_frontier_workspace_bytes", "pic_frontier_prefill_attn",
            "pic_decode_workspace_bytes", "pic_decode_attn", "pic_decode_attn_rope", "pic_status_string",
            "pic_last_error",
-           "pic_decode_auto_splits", "pic_decode_attn_noalloc")
+           "pic_decode_auto_splits", "pic_decode_attn_noalloc",
+           "pic_page_grow", "pic_page_fork", "pic_page_free", "pic_page_compact", "pic_page_blocks", "pic_page_copy",
+           "pic_page_suffix_attn", "pic_page_suffix_attn_rope", "pic_page_decode_attn", "pic_page_decode_attn_rope")
 PIC_DECODE_SCRATCH_BYTES = 8 << 20
 
 
@@ -65,6 +67,16 @@ class Model(ctypes.Structure):
                      self.rope_pairing, n if self.rope_tables > 1 else self.rope_tables)
 
 
+class Pages(ctypes.Structure):
+    """pic_pages: n_pages pages of page_tokens tokens per (layer, kv head), table_cap page table
+    entries per request."""
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("table_cap", ctypes.c_int32)]
+
+    @classmethod
+    def of(cls, n_pages, page_tokens, table_cap):
+        return cls(int(n_pages), int(page_tokens), int(table_cap))
+
+
 BLOCK_DTYPE = np.dtype([("request", np.int32), ("src_token", np.int32), ("dst_slot", np.int32),
                         ("n_tokens", np.int32), ("delta", np.int32)])
 
@@ -80,7 +92,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         raise ImportError(f"{path} is missing: build it with `python -m paper_2607_28069_amd.build`")
     lib = ctypes.CDLL(path)
     P, I32, I64, SZ, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
-    MP = ctypes.POINTER(Model)
+    MP, PP = ctypes.POINTER(Model), ctypes.POINTER(Pages)
     sig = {
         "pic_plan_layout": (ctypes.c_int, [I32, P, P, I32, P, P, P, I64, P, I32, P, P]),
         "pic_plan_frontier": (ctypes.c_int, [I32, P, P, I32, P, P, P, I64, P, I32, P, P, P, I32, P]),
@@ -111,6 +123,18 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "pic_last_error": (ctypes.c_char_p, []),
         "pic_decode_auto_splits": (I32, [MP, I32, I32]),
         "pic_decode_attn_noalloc": (ctypes.c_int, [MP, P, P, P, P, P, I32, I32, P, I32, I32, F, I32, P, P]),
+        "pic_page_grow": (ctypes.c_int, [PP, I32, P, P, P, P, P, I32, P]),
+        "pic_page_fork": (ctypes.c_int, [PP, I32, P, P, I32, I32, I32]),
+        "pic_page_free": (ctypes.c_int, [PP, I32, P, P, I32, I32]),
+        "pic_page_compact": (ctypes.c_int, [PP, I32, P, P, P, I32, P, P]),
+        "pic_page_blocks": (ctypes.c_int, [PP, I32, P, P, I32, P, I32, P]),
+        "pic_page_copy": (ctypes.c_int, [MP, PP, P, P, P, I32, P]),
+        "pic_page_suffix_attn": (ctypes.c_int, [MP, PP, P, P, P, P, P, P, I32, P, I32, P, I32, F, P, P, SZ, P]),
+        "pic_page_suffix_attn_rope": (ctypes.c_int, [MP, PP, P, P, P, P, P, P, I32, P, I32, P, I32, P, I32, F, P, P,
+                                                     SZ, P]),
+        "pic_page_decode_attn": (ctypes.c_int, [MP, PP, P, P, P, P, P, P, I32, P, I32, I32, F, I32, P, P, SZ, P]),
+        "pic_page_decode_attn_rope": (ctypes.c_int, [MP, PP, P, P, P, P, P, P, I32, P, I32, I32, P, I32, F, I32, P, P,
+                                                     SZ, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -384,6 +408,141 @@ def pic_decode_attn_noalloc(model: Model, q, k_new, v_new, cache_k, cache_v, bat
                                           _ptr(cache_k), _ptr(cache_v), int(batch), int(cache_cap),
                                           _ptr(base_len), int(step), int(max_base_len), float(scale),
                                           int(n_splits), _ptr(out), _stream(stream)))
+
+
+def _host_state(a, n, name):
+    """Address of a host int32 array of n entries that the call updates in place."""
+    if not isinstance(a, np.ndarray) or a.dtype != np.int32 or not a.flags.c_contiguous or not a.flags.writeable:
+        raise ValueError(f"{name}: a writeable contiguous numpy int32 array is updated in place")
+    if a.size != n:
+        raise ValueError(f"{name}: {a.size} entries, {n} expected")
+    return a.ctypes.data
+
+
+def _page_state(pages, refs, page_table, batch):
+    return _host_state(refs, pages.n_pages, "refs"), _host_state(page_table, batch * pages.table_cap, "page_table")
+
+
+def pic_page_grow(pages: Pages, refs, page_table, length, new_length) -> np.ndarray:
+    """Room for slots [length[b], new_length[b]) of every request; refs [n_pages] and page_table
+    [batch][table_cap] (numpy int32) are updated.  Returns the (source, destination) page pairs to
+    copy (pic_page_copy) before anything is stored."""
+    ln, p_len = _host_i32(length)
+    nl, p_new = _host_i32(new_length)
+    if len(ln) != len(nl):
+        raise ValueError("length and new_length differ in size")
+    p_refs, p_table = _page_state(pages, refs, page_table, len(ln))
+    pairs, n = np.zeros((max(len(ln), 1), 2), np.int32), ctypes.c_int32(0)
+    _check(load().pic_page_grow(ctypes.byref(pages), len(ln), p_refs, p_table, p_len, p_new, pairs.ctypes.data,
+                                len(pairs), ctypes.byref(n)))
+    return pairs[: n.value]
+
+
+def pic_page_fork(pages: Pages, batch, refs, page_table, src, length, dst):
+    """Request dst (holding no page) shares the pages of src's first `length` slots."""
+    _check(load().pic_page_fork(ctypes.byref(pages), int(batch), *_page_state(pages, refs, page_table, batch), int(src),
+                                int(length), int(dst)))
+
+
+def pic_page_free(pages: Pages, batch, refs, page_table, request, keep_len=0):
+    """Lets go of a request's pages past its first keep_len slots."""
+    _check(load().pic_page_free(ctypes.byref(pages), int(batch), *_page_state(pages, refs, page_table, batch),
+                                int(request), int(keep_len)))
+
+
+def pic_page_compact(pages: Pages, batch, refs, page_table):
+    """Renumbers the pages in use to [0, n_used).  Returns (page pairs to copy, n_used)."""
+    p_refs, p_table = _page_state(pages, refs, page_table, batch)
+    pairs = np.zeros((pages.n_pages // 2 + 1, 2), np.int32)
+    n, used = ctypes.c_int32(0), ctypes.c_int32(0)
+    _check(load().pic_page_compact(ctypes.byref(pages), int(batch), p_refs, p_table, pairs.ctypes.data, len(pairs),
+                                   ctypes.byref(n), ctypes.byref(used)))
+    return pairs[: n.value], used.value
+
+
+def pic_page_blocks(pages: Pages, page_table, blocks) -> np.ndarray:
+    """Gather blocks (pic_plan_layout / pic_plan_frontier) as blocks of the paged buffers: for pic_compose
+    and pic_compose_shared with the pages as caches, batch 1 and cache_cap n_pages * page_tokens."""
+    table, p_table = _host_i32(page_table)
+    if table.ndim != 2 or table.shape[1] != pages.table_cap:
+        raise ValueError("page_table: [batch][table_cap] expected")
+    blocks = np.ascontiguousarray(blocks, BLOCK_DTYPE)
+    n = ctypes.c_int32(0)
+    call = lambda out, cap: load().pic_page_blocks(ctypes.byref(pages), len(table), p_table, blocks.ctypes.data,
+                                                   len(blocks), out, cap, ctypes.byref(n))
+    st = call(None, 0)
+    if st not in (0, -4):
+        _check(st)
+    out = np.zeros(max(n.value, 1), BLOCK_DTYPE)
+    _check(call(out.ctypes.data, len(out)))
+    return out[: n.value]
+
+
+def _same_device(*tensors):
+    """The launch goes to the current device: tensors of another one are refused."""
+    import torch
+    at = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"tensor on device {t.get_device()}, the current one is {at}")
+
+
+def pic_page_copy(model: Model, pages: Pages, pages_k, pages_v, pairs, stream=None):
+    """pairs: host [n][2] (source, destination) pages; copied in every layer and kv head of both buffers."""
+    pairs, p_pairs = _host_i32(pairs)
+    if pairs.size and (pairs.ndim != 2 or pairs.shape[1] != 2):
+        raise ValueError("pairs: [n][2] expected")
+    k, v = _ptr(pages_k), _ptr(pages_v)
+    _same_device(pages_k, pages_v)
+    _check(load().pic_page_copy(ctypes.byref(model), ctypes.byref(pages), k, v, p_pairs, pairs.size // 2,
+                                _stream(stream)))
+
+
+def _page_args(model, pages, tensors, page_table, batch, lens):
+    """The leading arguments of the attention calls over pages."""
+    args = [_ptr(t) for t in tensors] + [_ptr(page_table), int(batch), _ptr(lens)]
+    _same_device(*tensors, page_table, lens)
+    return (ctypes.byref(model), ctypes.byref(pages), *args)
+
+
+def pic_page_suffix_attn(model: Model, pages: Pages, q, k_suf, v_suf, pages_k, pages_v, page_table, batch, ctx_len,
+                         max_ctx, n_suffix, out, workspace=None, n_valid=None, scale=0.0, stream=None):
+    """page_table: device int32 [batch][table_cap]; n_valid: None, or device int32 [batch] tokens used."""
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    args = _page_args(model, pages, (q, k_suf, v_suf, pages_k, pages_v), page_table, batch, ctx_len)
+    _check(load().pic_page_suffix_attn(*args, int(max_ctx), _ptr(n_valid), int(n_suffix), float(scale), _ptr(out),
+                                       _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pic_page_suffix_attn_rope(model: Model, pages: Pages, q, k_suf, v_suf, pages_k, pages_v, page_table, batch, ctx_len,
+                              max_ctx, n_suffix, table, max_abs_delta, out, workspace=None, n_valid=None, scale=0.0,
+                              stream=None):
+    """q / k_suf unrotated: turned to positions ctx_len[b] + i inside the kernel."""
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    args = _page_args(model, pages, (q, k_suf, v_suf, pages_k, pages_v), page_table, batch, ctx_len)
+    _check(load().pic_page_suffix_attn_rope(*args, int(max_ctx), _ptr(n_valid), int(n_suffix), _ptr(table),
+                                            int(max_abs_delta), float(scale), _ptr(out), _ptr(workspace), ws_bytes,
+                                            _stream(stream)))
+
+
+def pic_page_decode_attn(model: Model, pages: Pages, q, k_new, v_new, pages_k, pages_v, page_table, batch, base_len,
+                         step, max_base_len, out, workspace=None, n_splits=0, scale=0.0, stream=None):
+    """page_table: device int32 [batch][table_cap]; a negative base_len marks padding of the batch."""
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    args = _page_args(model, pages, (q, k_new, v_new, pages_k, pages_v), page_table, batch, base_len)
+    _check(load().pic_page_decode_attn(*args, int(step), int(max_base_len), float(scale), int(n_splits), _ptr(out),
+                                       _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pic_page_decode_attn_rope(model: Model, pages: Pages, q, k_new, v_new, pages_k, pages_v, page_table, batch,
+                              base_len, step, max_base_len, table, max_abs_delta, out, workspace=None, n_splits=0,
+                              scale=0.0, stream=None):
+    """q / k_new unrotated: turned to position base_len[b] + step inside the kernel."""
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    args = _page_args(model, pages, (q, k_new, v_new, pages_k, pages_v), page_table, batch, base_len)
+    _check(load().pic_page_decode_attn_rope(*args, int(step), int(max_base_len), _ptr(table), int(max_abs_delta),
+                                            float(scale), int(n_splits), _ptr(out), _ptr(workspace), ws_bytes,
+                                            _stream(stream)))
 
 
 def pic_status_string(status: int) -> str:

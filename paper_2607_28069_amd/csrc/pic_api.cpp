@@ -10,13 +10,12 @@
 #include <vector>
 
 #include "pic.h"
+#include "pic_check.h"
 #include "pic_internal.h"
 
-#define PIC_API extern "C" __attribute__((visibility("default")))
+namespace pic {
 
-namespace {
-
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
 pic_status fail(pic_status st, const char* fmt, ...) {
   char buf[512];
@@ -39,12 +38,6 @@ pic_status hip_status(hipError_t e, const char* what) {
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-#define PIC_CHECK(expr)              \
-  do {                               \
-    pic_status _s = (expr);          \
-    if (_s != PIC_OK) return _s;     \
-  } while (0)
 
 pic_status check_ptr(const void* p, const char* name) {
   if (p == nullptr) return fail(PIC_ERR_INVALID_ARG, "%s is NULL", name);
@@ -74,14 +67,7 @@ pic_status check_model(const pic_model* m) {
 
 int32_t n_tables(const pic_model* m) { return m->rope_tables > 1 ? m->rope_tables : 1; }
 
-constexpr int32_t kMaxAbsDelta = 1 << 20;
-// Rows one re-rotation call may cover: their element offsets stay far inside int64.
-constexpr int64_t kMaxRerotateRows = int64_t(1) << 48;
-// The bf16 attention kernels address a cache stream (one layer, request and kv head), one
-// request's suffix rows and a pool head (one layer and kv head) with 32-bit byte offsets from
-// a buffer base: each must stay under 2^32 bytes (rows of 256 bytes).
-constexpr int64_t kMaxRows32 = (int64_t(1) << 32) / 256 - 1;
-static pic_status check_rows32(int64_t cache_cap, int64_t suffix_rows, int64_t pool_tokens) {
+pic_status check_rows32(int64_t cache_cap, int64_t suffix_rows, int64_t pool_tokens) {
   if (cache_cap > kMaxRows32 || suffix_rows > kMaxRows32 || pool_tokens > kMaxRows32)
     return fail(PIC_ERR_UNSUPPORTED,
                 "a cache stream, a request's suffix rows or a pool head exceeds %lld rows",
@@ -89,9 +75,7 @@ static pic_status check_rows32(int64_t cache_cap, int64_t suffix_rows, int64_t p
   return ok();
 }
 
-size_t elem_bytes(const pic_model* m) { return m->dtype == PIC_F32 ? 4 : 2; }
-
-float scale_log2_of(const pic_model* m, float scale) {
+static float scale_log2_of(const pic_model* m, float scale) {
   const double s = scale == 0.f ? 1.0 / std::sqrt((double)m->head_dim) : (double)scale;
   return (float)(s * 1.4426950408889634);  // log2(e)
 }
@@ -108,19 +92,12 @@ pic::AttnShape shape_of(const pic_model* m, int32_t batch, int32_t cache_cap, fl
   return s;
 }
 
-pic_status check_attn_model(const pic_model* m) { return check_model(m); }
-
-// bf16 caches run on the matrix-core kernels (prefill in every mode and decode, head_dim 128 or
-// 64); float32 caches on the float32 kernel.
-bool mfma_prefill(const pic_model* m) { return m->dtype == PIC_BF16; }
-bool mfma_decode(const pic_model* m) { return m->dtype == PIC_BF16; }
-
 // The workspace of a prefill of n_suffix tokens after max_ctx: what the query call says.  A launch
 // that fills half the GPU can do without and runs whole then; a workspace that is not aligned
 // counts as not brought there (it is not needed), and is refused where it is needed.
 pic_status check_prefill_workspace(const pic_model* m, int32_t batch, int32_t n_suffix, int32_t max_ctx,
                                    const void* workspace, size_t* ws_bytes) {
-  if (!mfma_prefill(m)) return PIC_OK;
+  if (m->dtype != PIC_BF16) return PIC_OK;   // (float32 attention takes none)
   const pic::AttnShape s = shape_of(m, batch, max_ctx + n_suffix, 0.f);
   if (workspace == nullptr) *ws_bytes = 0;
   if (pic::prefill_bf16_may_run_whole(s, n_suffix)) {
@@ -131,6 +108,62 @@ pic_status check_prefill_workspace(const pic_model* m, int32_t batch, int32_t n_
   if (*ws_bytes < need) return fail(PIC_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, *ws_bytes);
   return need > 0 ? check_ptr(workspace, "workspace") : PIC_OK;
 }
+
+// The split count of a decode call and where its partials go: *n_splits 0 picks one; use_scratch: the
+// library's per-device array instead of the caller's workspace.
+pic_status plan_decode_call(const pic_model* model, const AttnShape& s, int32_t max_len, bool use_scratch,
+                            int32_t* n_splits_io, void** workspace_io, size_t* ws_bytes_io) {
+  int32_t n_splits = *n_splits_io;
+  void* workspace = *workspace_io;
+  size_t ws_bytes = *ws_bytes_io;
+  if (n_splits == 0) {
+    // (a launch that fills the GPU whole leaves the scratch array alone: such calls may overlap)
+    n_splits = decode_bf16_auto_splits(s, max_len);
+    const size_t held = use_scratch || !workspace || !aligned16(workspace) ? 0 : ws_bytes;
+    if (decode_bf16_workspace(s, max_len, n_splits) > held && decode_bf16_may_run_whole(s))
+      n_splits = 1;
+  }
+  if ((int64_t)n_splits * s.batch * model->n_kv_heads * ((model->n_q_heads / model->n_kv_heads + 15) / 16) > INT32_MAX)
+    return fail(PIC_ERR_UNSUPPORTED, "too many splits");
+  if (n_splits > max_len) n_splits = max_len;
+  const size_t need = decode_bf16_workspace(s, max_len, n_splits);
+  if (use_scratch) {
+    workspace = nullptr;
+    ws_bytes = 0;
+    if (need > decode_scratch_bytes())
+      return fail(PIC_ERR_WORKSPACE,
+                  "%d splits need %zu bytes of partials; the allocation-free decode holds %zu "
+                  "(pass fewer splits, or use pic_decode_attn with a workspace)",
+                  n_splits, need, decode_scratch_bytes());
+    if (need > 0) {
+      PIC_CHECK(hip_status(decode_scratch_ptr(&workspace), "decode scratch lookup"));
+      ws_bytes = decode_scratch_bytes();
+    }
+  }
+  if (need > 0 && (workspace == nullptr || ws_bytes < need))
+    return fail(PIC_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, ws_bytes);
+  if (need > 0) PIC_CHECK(check_ptr(workspace, "workspace"));
+  *n_splits_io = n_splits;
+  *workspace_io = workspace;
+  *ws_bytes_io = ws_bytes;
+  return PIC_OK;
+}
+
+}  // namespace pic
+
+using namespace pic;
+
+namespace {
+
+// Rows one re-rotation call may cover: their element offsets stay far inside int64.
+constexpr int64_t kMaxRerotateRows = int64_t(1) << 48;
+
+pic_status check_attn_model(const pic_model* m) { return check_model(m); }
+
+// bf16 caches run on the matrix-core kernels (prefill in every mode and decode, head_dim 128 or
+// 64); float32 caches on the float32 kernel.
+bool mfma_prefill(const pic_model* m) { return m->dtype == PIC_BF16; }
+bool mfma_decode(const pic_model* m) { return m->dtype == PIC_BF16; }
 
 // Attention over a float32 cache: n_q query rows per request at the positions `pos` gives them.
 // k_new / v_new: the call's own tokens, to be stored too (NULL: already in the cache).
@@ -850,33 +883,7 @@ pic_status decode_impl(const pic_model* model, const void* q, const void* k_new,
     pos.offset = step;
     return launch_f32(s, q, k_new, v_new, cache_k, cache_v, pos, 1, out, st, "decode attention launch");
   }
-  if (n_splits == 0) {
-    // (a launch that fills the GPU whole leaves the scratch array alone: such calls may overlap)
-    n_splits = pic::decode_bf16_auto_splits(s, (int32_t)max_len);
-    const size_t held = use_scratch || !workspace || !aligned16(workspace) ? 0 : ws_bytes;
-    if (pic::decode_bf16_workspace(s, (int32_t)max_len, n_splits) > held && pic::decode_bf16_may_run_whole(s))
-      n_splits = 1;
-  }
-  if ((int64_t)n_splits * batch * model->n_kv_heads * ((model->n_q_heads / model->n_kv_heads + 15) / 16) > INT32_MAX)
-    return fail(PIC_ERR_UNSUPPORTED, "too many splits");
-  if (n_splits > max_len) n_splits = (int32_t)max_len;
-  const size_t need = pic::decode_bf16_workspace(s, (int32_t)max_len, n_splits);
-  if (use_scratch) {
-    workspace = nullptr;
-    ws_bytes = 0;
-    if (need > pic::decode_scratch_bytes())
-      return fail(PIC_ERR_WORKSPACE,
-                  "%d splits need %zu bytes of partials; the allocation-free decode holds %zu "
-                  "(pass fewer splits, or use pic_decode_attn with a workspace)",
-                  n_splits, need, pic::decode_scratch_bytes());
-    if (need > 0) {
-      PIC_CHECK(hip_status(pic::decode_scratch_ptr(&workspace), "decode scratch lookup"));
-      ws_bytes = pic::decode_scratch_bytes();
-    }
-  }
-  if (need > 0 && (workspace == nullptr || ws_bytes < need))
-    return fail(PIC_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, ws_bytes);
-  if (need > 0) PIC_CHECK(check_ptr(workspace, "workspace"));
+  PIC_CHECK(plan_decode_call(model, s, (int32_t)max_len, use_scratch, &n_splits, &workspace, &ws_bytes));
   return hip_status(pic::launch_decode_bf16(s, static_cast<const pic::bf16_t*>(q),
                                             static_cast<const pic::bf16_t*>(k_new),
                                             static_cast<const pic::bf16_t*>(v_new),

@@ -82,6 +82,35 @@ PIC_HD bool tile_run_ok(int32_t src, int32_t delta, int32_t s0, int32_t ctx, int
          delta <= max_abs_delta && s0 + PIC_BLOCK_TOKENS <= ctx;
 }
 
+// ---- Paged caches: slot t of request b lives in row page * P + t % P of its (layer, kv head)
+// stream, page = table[b][t / P], P = 1 << shift; a stream holds n_pages * P rows.
+struct PageMap {
+  const int32_t* table = nullptr;   // [batch][cap]
+  int32_t cap = 0, n_pages = 0, shift = 0;
+};
+// Entry i of a request's page table, as a page to read: clamped into the table and the pages.
+PIC_HD int32_t clamp_entry(int32_t i, const PageMap& m) { return clamp_i32(i, 0, m.cap - 1); }
+PIC_HD int32_t clamp_page(int32_t page, const PageMap& m) { return clamp_i32(page, 0, m.n_pages - 1); }
+// The row `slot` of request b is read from (slot >= 0).
+PIC_HD int64_t page_row(const PageMap& m, int32_t b, int32_t slot) {
+  const int32_t page = clamp_page(m.table[(int64_t)b * m.cap + clamp_entry(slot >> m.shift, m)], m);
+  return ((int64_t)page << m.shift) + (slot & ((1 << m.shift) - 1));
+}
+// The row `slot` of request b is stored to, -1 where the table gives it no page.
+PIC_HD int64_t page_store_row(const PageMap& m, int32_t b, int32_t slot) {
+  const int32_t i = slot >> m.shift;
+  if (i < 0 || i >= m.cap) return -1;
+  const int32_t page = m.table[(int64_t)b * m.cap + i];
+  if (page < 0 || page >= m.n_pages) return -1;
+  return ((int64_t)page << m.shift) + (slot & ((1 << m.shift) - 1));
+}
+// New tokens of request b that a call over pages uses: none where its length is negative (padding
+// of the batch), else n_valid[b] of the n_new, or all of them.
+PIC_HD int32_t page_new_tokens(const int32_t* base_len, const int32_t* n_valid, int32_t b, int32_t n_new) {
+  if (base_len[b] < 0) return 0;
+  return n_valid ? clamp_len(n_valid[b], n_new) : n_new;
+}
+
 // ---- Split decode: the key ranges of a batch of uneven contexts ----
 // A split launch has n_splits workgroups per (request, kv head).  They are dealt to the requests
 // by length: request b of u_b units (kDecodeUnit keys each, the last one partial) gets

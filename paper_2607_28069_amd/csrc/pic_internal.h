@@ -122,6 +122,38 @@ struct F32AttnArgs {
 };
 hipError_t launch_attn_f32(const F32AttnArgs& a);
 
+// Attention of n_new new tokens per request over a paged cache (s.cache_cap = rows of a stream): token
+// i of request b sits at min(base_len[b], max_base) + offset + i, for i < page_new_tokens(b); its
+// K/V are stored and it attends over every slot up to its own.  With a rotary table (bf16) q and k_new
+// arrive unrotated.
+struct PageAttnArgs {
+  AttnShape s;
+  PageMap map;
+  const void* q = nullptr;
+  const void* k_new = nullptr;
+  const void* v_new = nullptr;
+  void* pages_k = nullptr;
+  void* pages_v = nullptr;
+  const int32_t* base_len = nullptr;
+  const int32_t* n_valid = nullptr;
+  int32_t max_base = 0, offset = 0, n_new = 0;
+  const float2* table = nullptr;
+  int64_t table_stride = 0;
+  int32_t max_abs_delta = 0;
+  bool interleaved = false;
+  void* out = nullptr;
+  void* workspace = nullptr;
+  size_t ws_bytes = 0;
+  int32_t n_splits = 0;
+  hipStream_t stream = nullptr;
+};
+hipError_t launch_page_attn(pic_dtype dt, const PageAttnArgs& a);
+
+// Page pairs[i][1] = page pairs[i][0] in each of the n_streams (layer, kv head) streams of both
+// buffers; pages of page_bytes bytes, n_pages per stream.  `pairs` is host memory, read before the call returns.
+hipError_t launch_page_copy(void* pages_k, void* pages_v, int64_t n_streams, int64_t n_pages, int64_t page_bytes,
+                            const int32_t* pairs, int32_t n_pairs, hipStream_t stream);
+
 size_t prefill_bf16_workspace(const AttnShape& s, int32_t n_suffix, int32_t max_ctx);
 // Launches that may bring less than that: they then run unsplit.
 bool prefill_bf16_may_run_whole(const AttnShape& s, int32_t n_suffix);

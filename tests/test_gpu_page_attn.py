@@ -1,0 +1,220 @@
+"""Attention over pages against the definition in 64 bits: decode and suffix prefill, every type, head
+layout and page size, lengths from one token on, padding of the batch, bad page tables."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_28069_amd as pic
+from page_path import DEV, SENTINEL, check, check_pages, decode, reference, rope_table, rows, setup, suffix
+
+pytestmark = pytest.mark.gpu
+
+HEADS = [(4, 2, 64), (32, 8, 128), (28, 4, 128), (5, 1, 64), (3, 3, 128), (40, 1, 128)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d", HEADS)
+@pytest.mark.parametrize("P", [16, 64, 256])
+def test_decode(dtype, hq, hkv, d, P):
+    x = setup(hq, hkv, d, dtype, P, [0, 1, 15, 16, 17, 63, 64, 65, 300, -1, 511], [1] * 11)
+    decode(x)
+    check(x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ctx", [[0], [1], [7], [31], [4097], [-1, 0, -1]])
+def test_decode_few_rows(dtype, ctx):
+    for P in (16, 128, 1024):
+        x = setup(8, 2, 128, dtype, P, ctx, [1] * len(ctx), slack=5)
+        decode(x, step=0)
+        check(x)
+
+
+@pytest.mark.parametrize("n_splits", [1, 2, 3, 8, 13, 64])
+@pytest.mark.parametrize("P", [16, 32, 64])
+def test_decode_splits(n_splits, P):
+    # uneven contexts, some shorter than the ranges a split gives them, padding in between
+    x = setup(16, 4, 128, "bf16", P, [3000, -1, 5, 1029, 8400, 0, -1, 4096], [1] * 8, slack=77)
+    decode(x, n_splits=n_splits)
+    check(x)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("base", [[-1, -1, -1], [9000, -1, 9000], [9000, 9000, 9000], [-1, 12000, 100], [12000, 12000, -1]])
+def test_decode_dealt_ranges_with_padding(d, base):
+    # 8 splits and long contexts: ranges dealt by length, padding gets none
+    x = setup(8, 2, d, "bf16", 64, base, [1, 1, 1], slack=12000 - max(max(base), 0))
+    decode(x, n_splits=8)
+    check(x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("step", [1, 40])
+def test_decode_step_and_layers(dtype, step):
+    x = setup(8, 4, 64, dtype, 32, [step, 100 + step, 77 + step], [1] * 3, L=3, slack=9)
+    decode(x, step=step, scale=0.07)
+    check(x, scale=0.07)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d", HEADS)
+@pytest.mark.parametrize("P", [16, 64, 256])
+def test_suffix(dtype, hq, hkv, d, P):
+    x = setup(hq, hkv, d, dtype, P, [0, 1, 63, 64, 65, -1, 200], [19, 1, 19, 7, 0, 19, 18], n=19)
+    suffix(x)
+    check(x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,ctx", [(1, [0]), (1, [4000, 3, 700]), (2, [31]), (64, [64, 0]), (65, [129]), (130, [500, 1000])])
+@pytest.mark.parametrize("P", [16, 128])
+def test_suffix_lengths(dtype, n, ctx, P):
+    x = setup(8, 2, 128, dtype, P, ctx, [n] * len(ctx), slack=3)
+    suffix(x, n_valid=None)
+    check(x)
+
+
+def test_suffix_all_padding():
+    for dtype in ("bf16", "f32"):
+        x = setup(4, 2, 64, dtype, 16, [-1, 50, 0], [9, 0, 0], n=9)
+        suffix(x)
+        check(x)
+
+
+def test_suffix_long_split_over_keys():
+    # one request: key ranges split over workgroups, with padding tokens at the end
+    for P, nv in ((16, 33), (64, 40)):
+        x = setup(32, 8, 128, "bf16", P, [9001, 20], [nv, 1], n=40)
+        assert pic.pic_prefill_workspace_bytes(x.model, x.B, x.n, x.max_ctx) > 0
+        suffix(x)
+        check(x)
+
+
+@pytest.mark.parametrize("kind", ["decode", "suffix"])
+@pytest.mark.parametrize("pairing", ["half", "interleaved"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rope_is_turning_first(kind, pairing, d):
+    """Unrotated rows in: bit for bit what turning them with pic_rerotate_keys first gives."""
+    ctx, new = [0, 17, 640, -1, 2000], [1] * 5 if kind == "decode" else [21, 3, 21, 21, 0]
+    n = 1 if kind == "decode" else 21
+    x = setup(8, 2, d, "bf16", 32, ctx, new, n=n, pairing=pairing, L=2)
+    y = setup(8, 2, d, "bf16", 32, ctx, new, n=n, pairing=pairing, L=2)
+    rope = rope_table(x)
+    call = decode if kind == "decode" else suffix
+    call(x, rope=rope)
+    pos = torch.tensor([[max(c, 0) + i for i in range(n)] for c in ctx], dtype=torch.int32, device=DEV)
+    for t, h in ((y.q, y.hq), (y.k, y.hkv)):
+        pic.pic_rerotate_keys(y.model, t, t, y.L * y.B * n, h, pos.repeat(y.L, 1, 1).contiguous(), *rope)
+    call(y)
+    assert (x.out == y.out).all()
+    for a, b in ((x.pk, y.pk), (x.pv, y.pv)):
+        assert (a.view(torch.int16) == b.view(torch.int16)).all()
+    for b in range(y.B):   # and those outputs are right
+        m = y.new[b] if ctx[b] >= 0 else 0
+        y.K[b] = torch.cat([y.K[b][:, :, : y.K[b].shape[2] - m], y.k[:, b, :m].transpose(1, 2)], 2)
+    check(y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_scores(dtype):
+    # scores far apart: one key takes all; the running maximum moves late
+    x = setup(4, 1, 128, dtype, 16, [700, 90], [1, 1])
+    for b, t in ((0, 699), (1, 3)):
+        x.pk[:, :, rows(x, b, t, t + 1)] *= 6
+        x.K[b][:, :, t] *= 6
+    x.q *= 4
+    decode(x)
+    check(x)
+
+
+@pytest.mark.parametrize("kind", ["decode", "suffix"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_bad_tables_stay_inside(kind, dtype):
+    """Entries outside the pages: some other page is read, nothing is stored there, and requests whose
+    entries are right keep their results."""
+    x = setup(8, 2, 64, dtype, 16, [50, 40, 100], [1, 1, 1] if kind == "decode" else [20, 20, 20])
+    for p in (x.pk, x.pv):
+        p[torch.isnan(p)] = 0
+    keep = x.pk.clone(), x.pv.clone()
+    bad = x.table.clone()
+    bad[0, :] = torch.tensor([-5, 2**31 - 1, x.pages.n_pages, -2**31, x.pages.n_pages + 5], device=DEV)[: bad.shape[1]].repeat(3)[: bad.shape[1]]
+    x.table = bad
+    (decode if kind == "decode" else suffix)(x)
+    torch.cuda.synchronize()
+    ref, _, _ = reference(x)
+    for b in (1, 2):
+        m = x.new[b]
+        err = (x.out[:, b, :m].double() - ref[:, b, :m]).norm() / ref[:, b, :m].norm()
+        assert err < (2.0 ** -8 if dtype == "bf16" else 2e-5)
+        r = rows(x, b, 0, x.K[b].shape[2])
+        for p, want in ((x.pk, x.K[b]), (x.pv, x.V[b])):
+            assert (p[:, :, r] == want).all()
+    for p, k in zip((x.pk, x.pv), keep):   # request 0 stored nothing
+        same = (p == k).all(-1).all(0).all(0)
+        stored = torch.zeros_like(same)
+        for b in (1, 2):
+            stored[rows(x, b, x.ctx[b], x.ctx[b] + x.new[b])] = True
+        assert (same | stored).all()
+
+
+def test_lengths_are_clamped():
+    # lengths above max_ctx: read as max_ctx
+    x = setup(8, 2, 128, "bf16", 16, [40, 33], [1, 1])
+    x.len = torch.tensor([2**31 - 1, 33], dtype=torch.int32, device=DEV)
+    decode(x)
+    check(x)
+    x = setup(8, 2, 128, "bf16", 16, [40, 33], [3, 3])
+    x.len = torch.tensor([1 << 20, 33], dtype=torch.int32, device=DEV)
+    x.n_valid = torch.tensor([2**31 - 1, 3], dtype=torch.int32, device=DEV)
+    suffix(x)
+    check(x)
+
+
+def test_rows_past_32_bits():
+    """Pages whose rows lie past 2^32 bytes and 2^31 elements of a stream."""
+    for dtype, P, n_pages in (("bf16", 64, 1 << 19), ("f32", 1024, 20000)):
+        x = setup(4, 1, 128, dtype, P, [200, 130], [1, 1])
+        low = x.table_host.copy()
+        high = np.where(low >= 0, n_pages - 1 - low, -1).astype(np.int32)
+        big = []
+        for p in (x.pk, x.pv):
+            t = torch.empty((1, 1, n_pages * P, 128), dtype=x.dt, device=DEV)
+            for e in range(x.pages.n_pages):
+                t[:, :, (n_pages - 1 - e) * P: (n_pages - e) * P] = p[:, :, e * P: (e + 1) * P]
+            big.append(t)
+        x.pk, x.pv = big
+        assert n_pages * P * 128 * x.pk.element_size() > 2**32
+        x.table_host, x.table = high, torch.from_numpy(high).to(DEV)
+        x.pages = pic.Pages.of(n_pages, P, x.pages.table_cap)
+        decode(x)
+        small = x.pk[:, :, (n_pages - 20) * P:].clone(), x.pv[:, :, (n_pages - 20) * P:].clone()
+        del big
+        x.pk, x.pv = small
+        x.table_host = np.where(high >= 0, high - (n_pages - 20), -1)
+        x.pages = pic.Pages.of(20, P, x.pages.table_cap)
+        ok = torch.zeros(20 * P, dtype=torch.bool, device=DEV)
+        for b in range(x.B):
+            ok[rows(x, b, 0, x.K[b].shape[2])] = True
+        x.pk[:, :, ~ok] = float("nan")
+        x.pv[:, :, ~ok] = float("nan")
+        check(x)
+
+
+def test_binding_refusals():
+    x = setup(4, 2, 64, "bf16", 16, [5], [1])
+    for name in ("q", "k", "pk", "table", "len"):
+        y = setup(4, 2, 64, "bf16", 16, [5], [1])
+        setattr(y, name, getattr(y, name).cpu())
+        with pytest.raises((ValueError, RuntimeError)):
+            decode(y)
+    y = setup(4, 2, 64, "bf16", 16, [5], [1])
+    y.q = y.q.expand(2, *y.q.shape[1:])
+    with pytest.raises(ValueError):
+        decode(y)
+    with pytest.raises(pic.PicError):
+        decode(x, n_splits=4, ws=None)
+    assert (x.out == SENTINEL).all()
+    decode(x)
+    check(x)
