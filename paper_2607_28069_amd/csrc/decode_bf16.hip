@@ -98,6 +98,8 @@ struct DecodeArgs {
   const float2* table;    // rope variant: [L or 1][max_abs_delta + 1][D/2] cos/sin rows
   int64_t table_stride;
   int32_t max_abs_delta;
+  PageMap map;            // paged cache: cache_k / cache_v are [L][Hkv][stream_rows][D] and cache_cap bounds
+  int32_t stream_rows;    // the slots of a request
 };
 
 // How the key ranges of a split launch are dealt to the requests (pic_bounds.h): worked out by
@@ -123,23 +125,28 @@ __device__ __forceinline__ int32_t ceil_div24(int32_t u, int32_t c, float inv) {
   const int32_t r = u - q * c;
   return q + (r > 0 ? 1 : 0) + (r > c ? 1 : 0) - (r <= -c ? 1 : 0);
 }
+// kPages: a negative length is padding of the batch and gets no range
+template <bool kPages>
 __device__ __forceinline__ SplitLens split_lens(const int32_t* base_len, int32_t batch, int32_t max_base, int32_t step,
                                                 int32_t cache_cap) {
   const int lane = threadIdx.x & 63;
   SplitLens x = {0, 0};
   if (lane < batch) {
-    x.base = clamp_len(base_len[lane], max_base);
-    x.u = decode_units(min(x.base + step + 1, cache_cap));
+    const int32_t len = base_len[lane];
+    x.base = clamp_len(len, max_base);
+    if (!kPages || len >= 0) x.u = decode_units(min(x.base + step + 1, cache_cap));
   }
   return x;
 }
 __device__ __forceinline__ bool all_of(const SplitLens& x, int32_t units, int32_t batch) {
   return __ballot((int)(threadIdx.x & 63) < batch && x.u != units) == 0;
 }
+template <bool kPages>
 __device__ __forceinline__ SplitDeal deal_splits(const SplitLens& x, int32_t batch, int32_t n_splits) {
   const int lane = threadIdx.x & 63;
   const int32_t u = x.u, u0 = __builtin_amdgcn_readfirstlane(u);
   if (all_of(x, u0, batch)) {
+    if (kPages && u0 == 0) return {kDecodeUnit, 0, 0};   // nothing but padding
     const int32_t s = min(n_splits, u0), cu = __builtin_amdgcn_readfirstlane(ceil_div24(u0, s, __builtin_amdgcn_rcpf((float)s)));
     return {cu * kDecodeUnit, __builtin_amdgcn_readfirstlane(ceil_div24(u0, cu, __builtin_amdgcn_rcpf((float)cu))), 0};
   }
@@ -219,7 +226,11 @@ __device__ __forceinline__ void rot_operand(u32x4 (&c)[Dims<HD>::kSteps], const 
 
 // grid (S * B * Hkv, L), 256 threads.  kDealt: ranges dealt by length (decode_dealt), else n_splits equal
 // ones (a kernel of its own: tested in the kernel, the choice cost launches of 1600 short contexts 1 %).
-template <int HD, bool kRope, bool kInterleaved, bool kDealt>
+// kPages: the cache is handed out in pages of 1 << shift >= 16 tokens.  A tile's two blocks of 16 keys
+// lie in one page each, so a wave needs two page numbers per tile; it holds the table's next 64
+// entries in a register (lane j: entry win + j) and takes them out with readlane, the 64 after those on
+// their way, so that no tile's loads wait for the table.
+template <int HD, bool kRope, bool kInterleaved, bool kDealt, bool kPages>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 decode_bf16_kernel(DecodeArgs a) {
   constexpr int kHD = HD, kRowBytes = Dims<HD>::kRowBytes, kVTileBytes = Dims<HD>::kVTileBytes;
@@ -243,7 +254,7 @@ decode_bf16_kernel(DecodeArgs a) {
     place = {a.n_splits, b * a.n_splits};
     base = clamp_len(a.base_len[b], a.max_base);
   } else {
-    const SplitLens lens = split_lens(a.base_len, a.batch, a.max_base, a.step, a.cache_cap);
+    const SplitLens lens = split_lens<kPages>(a.base_len, a.batch, a.max_base, a.step, a.cache_cap);
     const int bg = at / a.eq.n;
     split = at % a.eq.n;
     b = bg / a.n_kv_heads;
@@ -251,7 +262,8 @@ decode_bf16_kernel(DecodeArgs a) {
     place = {a.eq.n, b * a.eq.n};
     chunk = a.eq.chunk;
     if (!all_of(lens, a.eq.units, a.batch)) {
-      const SplitDeal deal = deal_splits(lens, a.batch, a.n_splits);
+      const SplitDeal deal = deal_splits<kPages>(lens, a.batch, a.n_splits);
+      if (kPages && deal.n == 0) return;   // (uniform) a batch of padding
       chunk = deal.chunk;
       if (deal.n >= 0) {
         b = at / (deal.n * a.n_kv_heads);
@@ -286,18 +298,46 @@ decode_bf16_kernel(DecodeArgs a) {
   const int c1 = min(c0 + sub, wc1);
 
   const int64_t bh_kv = (((int64_t)l * a.batch + b) * a.n_kv_heads + g);
-  const bf16_t* Kg = a.cache_k + bh_kv * a.cache_cap * kHD;
-  const bf16_t* Vg = a.cache_v + bh_kv * a.cache_cap * kHD;
+  const int64_t row0 = kPages ? ((int64_t)l * a.n_kv_heads + g) * a.stream_rows : bh_kv * a.cache_cap;
+  const bf16_t* Kg = a.cache_k + row0 * kHD;
+  const bf16_t* Vg = a.cache_v + row0 * kHD;
   const bf16_t* Kn = a.k_new + bh_kv * kHD;
   const bf16_t* Vn = a.v_new + bh_kv * kHD;
+
+  // pages: entries [win, win + 64) and the 64 after them, for a range from slot `first` on (which does
+  // not wait for the lengths); the page of the new token, for its store at the end
+  const int32_t* ptab = kPages ? a.map.table + (int64_t)b * a.map.cap : nullptr;
+  int32_t win = 0, w_cur = 0, w_next = 0;
+  int64_t store_row = -1;
+  auto entry = [&](int32_t i) { return ptab[clamp_entry(i, a.map)]; };
+  if constexpr (kPages) {
+    const int64_t first = min((int64_t)split * chunk + wave * sub, (int64_t)a.cache_cap - 1);
+    win = (int32_t)(first >> a.map.shift);
+    w_cur = entry(win + lane);
+    w_next = entry(win + 64 + lane);
+    if constexpr (!kDealt) {
+      if (a.base_len[b] < 0) return;   // (uniform) padding of the batch
+    }
+  }
+  // the row that slot k0, a multiple of 16 (k0 >= the last one asked for), lies in
+  auto page_at = [&](int k0) -> int32_t {   // k0 uniform
+    const int32_t i = k0 >> a.map.shift;
+    if (i >= win + 64) {
+      win += 64;
+      w_cur = w_next;
+      w_next = entry(win + 64 + lane);
+    }
+    const int32_t page = clamp_page(__builtin_amdgcn_readlane(w_cur, i - win), a.map);
+    return (page << a.map.shift) + (k0 & ((1 << a.map.shift) - 1));
+  };
 
   // The workgroup holding slot p writes the new token into the cache.  Nobody reads that row
   // from the cache during this launch: the wave whose range holds it reads k_new / v_new.
   const float2* trow = kRope ? a.table + (int64_t)l * a.table_stride + (int64_t)min(p, a.max_abs_delta) * (kHD / 2)
                              : nullptr;   // rope variant: cos/sin of position p
-  if (hgrp == 0 && p < a.cache_cap && p >= wc0 && p < wc1 && wave == 0 && lane < 2 * KC) {
+  auto store_new = [&](int64_t row) {
     const int c = lane & (KC - 1);   // lanes [0, KC): K chunks, [KC, 2 KC): V chunks
-    u32x4* dst = reinterpret_cast<u32x4*>((lane < KC ? a.cache_k : a.cache_v) + (bh_kv * a.cache_cap + p) * kHD);
+    u32x4* dst = reinterpret_cast<u32x4*>((lane < KC ? a.cache_k : a.cache_v) + row * kHD);
     if (kRope && lane < KC) {   // the new key turned to p: lane c < KC/2 takes a chunk pair
       if (c < KC / 2) {
         // rotate-half: chunks c, c + KC/2 (frequencies 8 c ..); interleaved: 2 c, 2 c + 1 (8 c ..)
@@ -321,6 +361,12 @@ decode_bf16_kernel(DecodeArgs a) {
     } else {
       dst[c] = reinterpret_cast<const u32x4*>(lane < KC ? Kn : Vn)[c];
     }
+  };
+  const bool stores = hgrp == 0 && p < a.cache_cap && p >= wc0 && p < wc1 && wave == 0 && lane < 2 * KC;
+  if constexpr (kPages) {   // (stored after the key loop: nothing there waits for the entry)
+    if (stores) store_row = page_store_row(a.map, b, p);
+  } else if (stores) {
+    store_new(row0 + p);
   }
 
   const int n = lane & 15, g4 = lane >> 4;
@@ -340,11 +386,22 @@ decode_bf16_kernel(DecodeArgs a) {
 
   // K of one tile, straight into the A-operand layout: [mb][ks] = row k0 + 16 mb + n, head
   // dims 32 ks + 8 g4 .. +8.  Rows past the range are clamped (their scores are masked).
+  // (pages: blk16[mb] = (slot, row) of the tile's blocks of 16 keys; a block past the range is its last
+  // block again)
+  int blk_slot[2] = {0, 0};
+  int32_t blk_row[2] = {0, 0};
+  auto find_blocks = [&](int k0) {
+#pragma unroll
+    for (int mb = 0; mb < 2; ++mb) {
+      blk_slot[mb] = min(k0 + 16 * mb, (c1 - 1) & ~15);
+      blk_row[mb] = page_at(blk_slot[mb]);
+    }
+  };
   auto load_k = [&](int k0, u32x4 (&kr)[2][KS]) {
 #pragma unroll
     for (int mb = 0; mb < 2; ++mb) {
-      const int row = min(k0 + 16 * mb + n, c1 - 1);
-      const bf16_t* src = row == p ? Kn : Kg + (int64_t)row * kHD;
+      const int row = min((kPages ? blk_slot[mb] : k0 + 16 * mb) + n, c1 - 1);
+      const bf16_t* src = row == p ? Kn : Kg + (kPages ? (int64_t)blk_row[mb] + (row - blk_slot[mb]) : (int64_t)row) * kHD;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
         kr[mb][ks] = *reinterpret_cast<const u32x4*>(src + 32 * ks + 8 * g4);
@@ -357,10 +414,11 @@ decode_bf16_kernel(DecodeArgs a) {
   auto load_v = [&](int k0, uint8_t* buf) {
 #pragma unroll
     for (int i = 0; i < kTile / RPM; ++i) {
-      const int rl = RPM * i + ld_r;
-      const int row = min(k0 + rl, c1 - 1);
+      const int rl = RPM * i + ld_r, mb = RPM * i / 16;
+      const int row = min(kPages ? blk_slot[mb] + (RPM * i & 15) + ld_r : k0 + rl, c1 - 1);
       const int c = ld_slot ^ v_swz<HD>(rl);
-      const bf16_t* src = (row == p ? Vn : Vg + (int64_t)row * kHD) + 8 * c;
+      const bf16_t* src =
+          (row == p ? Vn : Vg + (kPages ? (int64_t)blk_row[mb] + (row - blk_slot[mb]) : (int64_t)row) * kHD) + 8 * c;
       __builtin_amdgcn_global_load_lds((const GLOBAL_AS void*)src,
                                        (LDS_AS void*)(buf + wave * kVTileBytes + RPM * i * kRowBytes), 16, 0,
                                        kNonTemporal);
@@ -395,6 +453,7 @@ decode_bf16_kernel(DecodeArgs a) {
     const uint8_t* vcur = P ? v_lds1 : v_lds0;
     uint8_t* vnext = P ? v_lds0 : v_lds1;
     if (k0 + kTile < c1) {
+      if constexpr (kPages) find_blocks(k0 + kTile);
       load_k(k0 + kTile, knext);
       load_v(k0 + kTile, vnext);
     }
@@ -456,6 +515,7 @@ decode_bf16_kernel(DecodeArgs a) {
 
   u32x4 k_a[2][KS], k_b[2][KS];
   if (c0 < c1) {
+    if constexpr (kPages) find_blocks(c0);
     load_k(c0, k_a);
     load_v(c0, v_lds0);
     __builtin_amdgcn_s_waitcnt(0x0F70);
@@ -463,6 +523,10 @@ decode_bf16_kernel(DecodeArgs a) {
       tile(k0, std::integral_constant<int, 0>{}, k_a, k_b);
       if (k0 + kTile < c1) tile(k0 + kTile, std::integral_constant<int, 1>{}, k_b, k_a);
     }
+  }
+
+  if constexpr (kPages) {
+    if (store_row >= 0) store_new(row0 + store_row);
   }
 
   // ---- merge the 4 waves (log-sum-exp) through LDS, reusing the V buffers
@@ -526,7 +590,7 @@ decode_bf16_kernel(DecodeArgs a) {
 // issued before any is used; the range groups then merge in LDS.  (One wave walking the ranges
 // took 4.9 us for 8 or 32 of them: a memory round trip per 8, once for the maxima and once for
 // the sums.)  A range that saw no key (maximum -inf) adds nothing.
-template <int HD, bool kDealt>
+template <int HD, bool kDealt, bool kPages>
 __global__ void __launch_bounds__(256) decode_combine_kernel(const float* __restrict__ ws_o,
                                                              const float* __restrict__ ws_ml,
                                                              const int32_t* __restrict__ base_len, int32_t batch,
@@ -553,15 +617,17 @@ __global__ void __launch_bounds__(256) decode_combine_kernel(const float* __rest
     }
   };
   if constexpr (kDealt) {
-    const SplitLens lens = split_lens(base_len, batch, max_base, step, cache_cap);
+    const SplitLens lens = split_lens<kPages>(base_len, batch, max_base, step, cache_cap);
     load(grp);   // (equal ranges fit the array whatever the lengths are)
     if (!all_of(lens, eq.units, batch)) {
-      place = place_of(deal_splits(lens, batch, n_splits), b);
+      place = place_of(deal_splits<kPages>(lens, batch, n_splits), b);
       load(grp);
     }
-    if (place.n == 1) return;   // (uniform) a whole request: its output is stored
+    // (uniform) a whole request: its output is stored; padding: there is none
+    if (kPages ? place.n <= 1 : place.n == 1) return;
   } else {
     load(grp);
+    if (kPages && base_len[b] < 0) return;   // (uniform) padding of the batch
   }
   float M = -INFINITY, den = 0.f;
   f32x4_t o = {};
@@ -601,21 +667,21 @@ __global__ void __launch_bounds__(256) decode_combine_kernel(const float* __rest
   reinterpret_cast<uint32_t*>(out + row * HD)[threadIdx.x] = pack_bf16x2(o0 * inv, o1 * inv);
 }
 
-template <int HD, bool kDealt>
+template <int HD, bool kDealt, bool kPages>
 hipError_t launch_decode_as(const DecodeArgs& a, dim3 grid, bool rope, bool interleaved, const AttnShape& s,
                             hipStream_t stream) {
   if (!rope)
-    hipLaunchKernelGGL((decode_bf16_kernel<HD, false, false, kDealt>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((decode_bf16_kernel<HD, false, false, kDealt, kPages>), grid, dim3(256), 0, stream, a);
   else if (interleaved)
-    hipLaunchKernelGGL((decode_bf16_kernel<HD, true, true, kDealt>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((decode_bf16_kernel<HD, true, true, kDealt, kPages>), grid, dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL((decode_bf16_kernel<HD, true, false, kDealt>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((decode_bf16_kernel<HD, true, false, kDealt, kPages>), grid, dim3(256), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_splits == 1) return e;
   // (a grid holds fewer than 2^32 threads per dimension)
   const int64_t rows = (int64_t)s.batch * s.n_q_heads, kPart = int64_t(1) << 23;
   for (int64_t row0 = 0; row0 < rows && e == hipSuccess; row0 += kPart) {
-    hipLaunchKernelGGL((decode_combine_kernel<HD, kDealt>), dim3((unsigned)std::min(rows - row0, kPart), s.n_layers),
+    hipLaunchKernelGGL((decode_combine_kernel<HD, kDealt, kPages>), dim3((unsigned)std::min(rows - row0, kPart), s.n_layers),
                        dim3(256), 0, stream, a.ws_o, a.ws_ml, a.base_len, s.batch, s.n_q_heads, a.max_base, a.step,
                        a.cache_cap, a.n_splits, a.eq, (int32_t)row0, a.out);
     e = hipGetLastError();
@@ -623,12 +689,12 @@ hipError_t launch_decode_as(const DecodeArgs& a, dim3 grid, bool rope, bool inte
   return e;
 }
 
-template <int HD>
+template <int HD, bool kPages>
 hipError_t launch_decode_hd(const DecodeArgs& a, dim3 grid, bool rope, bool interleaved, const AttnShape& s,
                             hipStream_t stream) {
   return decode_dealt(a.n_splits, a.batch, a.max_base + a.step + 1)
-             ? launch_decode_as<HD, true>(a, grid, rope, interleaved, s, stream)
-             : launch_decode_as<HD, false>(a, grid, rope, interleaved, s, stream);
+             ? launch_decode_as<HD, true, kPages>(a, grid, rope, interleaved, s, stream)
+             : launch_decode_as<HD, false, kPages>(a, grid, rope, interleaved, s, stream);
 }
 
 }  // namespace
@@ -656,49 +722,80 @@ hipError_t decode_scratch_ptr(void** out) {
   return hipSuccess;
 }
 
+namespace {
+
+// `a` as far as a call's buffers and lengths go; fills in what follows from the shape, and launches.
+template <bool kPages>
+hipError_t launch_decode(DecodeArgs a, const AttnShape& s, int32_t n_splits, void* workspace, bool interleaved,
+                         hipStream_t stream) {
+  if (s.batch == 0 || s.n_layers == 0) return hipSuccess;
+  const int32_t max_len = a.max_base + a.step + 1;
+  const size_t rows = (size_t)s.n_layers * s.batch * s.n_q_heads * n_splits;
+  a.ws_o = static_cast<float*>(workspace);
+  a.ws_ml = a.ws_o ? a.ws_o + rows * s.head_dim : nullptr;
+  a.batch = s.batch;
+  a.n_q_heads = s.n_q_heads;
+  a.n_kv_heads = s.n_kv_heads;
+  a.n_splits = n_splits;
+  const int32_t chunk = ceil_div(max_len, n_splits);
+  a.chunk = (int32_t)min((int64_t)decode_units(chunk) * kDecodeUnit, (int64_t)INT32_MAX / kDecodeUnit * kDecodeUnit);
+  a.eq = {};
+  if (decode_dealt(n_splits, s.batch, max_len)) {
+    a.eq.units = decode_units(std::min(max_len, a.cache_cap));
+    const int32_t per = ceil_div(a.eq.units, std::min(n_splits, a.eq.units));   // units per range
+    a.eq.n = ceil_div(a.eq.units, per);
+    a.eq.chunk = per * kDecodeUnit;
+  }
+  a.scale_log2 = s.scale_log2;
+  a.head_groups = decode_head_groups(s);
+  const dim3 grid(a.head_groups * n_splits * s.batch * s.n_kv_heads, s.n_layers);
+  if (s.head_dim == 64) return launch_decode_hd<64, kPages>(a, grid, a.table != nullptr, interleaved, s, stream);
+  return launch_decode_hd<128, kPages>(a, grid, a.table != nullptr, interleaved, s, stream);
+}
+
+}  // namespace
+
 hipError_t launch_decode_bf16(const AttnShape& s, const bf16_t* q, const bf16_t* k_new,
                               const bf16_t* v_new, bf16_t* cache_k, bf16_t* cache_v,
                               const int32_t* base_len, int32_t max_base, int32_t step,
                               int32_t n_splits, bf16_t* out, void* workspace, size_t,
                               const float2* rope_table, int64_t table_stride, int32_t max_abs_delta,
                               bool interleaved, hipStream_t stream) {
-  if (s.batch == 0 || s.n_layers == 0) return hipSuccess;
-  const int32_t max_len = max_base + step + 1;
-  DecodeArgs a;
+  DecodeArgs a = {};
   a.q = q;
   a.k_new = k_new;
   a.v_new = v_new;
   a.cache_k = cache_k;
   a.cache_v = cache_v;
+  a.cache_cap = s.cache_cap;
   a.base_len = base_len;
   a.out = out;
-  const size_t rows = (size_t)s.n_layers * s.batch * s.n_q_heads * n_splits;
-  a.ws_o = static_cast<float*>(workspace);
-  a.ws_ml = a.ws_o ? a.ws_o + rows * s.head_dim : nullptr;
-  a.batch = s.batch;
-  a.cache_cap = s.cache_cap;
-  a.n_q_heads = s.n_q_heads;
-  a.n_kv_heads = s.n_kv_heads;
   a.max_base = max_base;
   a.step = step;
-  a.n_splits = n_splits;
-  const int32_t chunk = ceil_div(max_len, n_splits);
-  a.chunk = (int32_t)min((int64_t)decode_units(chunk) * kDecodeUnit, (int64_t)INT32_MAX / kDecodeUnit * kDecodeUnit);
-  a.eq = {};
-  if (decode_dealt(n_splits, s.batch, max_len)) {
-    a.eq.units = decode_units(std::min(max_len, s.cache_cap));
-    const int32_t per = ceil_div(a.eq.units, std::min(n_splits, a.eq.units));   // units per range
-    a.eq.n = ceil_div(a.eq.units, per);
-    a.eq.chunk = per * kDecodeUnit;
-  }
-  a.scale_log2 = s.scale_log2;
   a.table = rope_table;
   a.table_stride = table_stride;
   a.max_abs_delta = max_abs_delta;
-  a.head_groups = decode_head_groups(s);
-  const dim3 grid(a.head_groups * n_splits * s.batch * s.n_kv_heads, s.n_layers);
-  if (s.head_dim == 64) return launch_decode_hd<64>(a, grid, rope_table != nullptr, interleaved, s, stream);
-  return launch_decode_hd<128>(a, grid, rope_table != nullptr, interleaved, s, stream);
+  return launch_decode<false>(a, s, n_splits, workspace, interleaved, stream);
+}
+
+hipError_t launch_decode_bf16_pages(const PageAttnArgs& p) {
+  DecodeArgs a = {};
+  a.q = static_cast<const bf16_t*>(p.q);
+  a.k_new = static_cast<const bf16_t*>(p.k_new);
+  a.v_new = static_cast<const bf16_t*>(p.v_new);
+  a.cache_k = static_cast<bf16_t*>(p.pages_k);
+  a.cache_v = static_cast<bf16_t*>(p.pages_v);
+  a.cache_cap = (int32_t)std::min((int64_t)p.map.cap << p.map.shift, (int64_t)INT32_MAX);
+  a.base_len = p.base_len;
+  a.out = static_cast<bf16_t*>(p.out);
+  a.max_base = p.max_base;
+  a.step = p.offset;
+  a.table = p.table;
+  a.table_stride = p.table_stride;
+  a.max_abs_delta = p.max_abs_delta;
+  a.map = p.map;
+  a.stream_rows = p.s.cache_cap;
+  return launch_decode<true>(a, p.s, p.n_splits, p.workspace, p.interleaved, p.stream);
 }
 
 }  // namespace pic

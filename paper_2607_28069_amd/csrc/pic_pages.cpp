@@ -395,7 +395,8 @@ pic_status page_attn(const pic_model* model, const pic_pages* pages, const void*
   a.ws_bytes = ws_bytes;
   a.n_splits = n_splits;
   a.stream = (hipStream_t)stream;
-  return hip_status(launch_page_attn(model->dtype, a), decode ? "page decode launch" : "page suffix launch");
+  if (decode) return hip_status(model->dtype == PIC_BF16 ? launch_decode_bf16_pages(a) : launch_page_attn(model->dtype, a), "page decode launch");
+  return hip_status(launch_page_attn(model->dtype, a), "page suffix launch");
 }
 
 }  // namespace

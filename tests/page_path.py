@@ -157,3 +157,14 @@ def check_pages(x):
     i = torch.int32 if x.dtype == "f32" else torch.int16
     for got, want in ((x.pk, want_k), (x.pv, want_v)):
         assert (got.view(i) == want.view(i)).all(), "page rows differ from the tokens they should hold"
+
+
+def contiguous(x, cap=None):
+    """The cached tokens (the new ones left out) as caches [L][B][Hkv][cap][D]; every other slot NaN."""
+    cap = cap or x.pages.table_cap * x.P
+    ck = torch.full((x.L, x.B, x.hkv, cap, x.d), float("nan"), dtype=x.dt, device=DEV)
+    cv = ck.clone()
+    for b in range(x.B):
+        m = x.ctx[b]
+        ck[:, b, :, :m], cv[:, b, :, :m] = x.K[b][:, :, :m], x.V[b][:, :, :m]
+    return ck, cv, cap

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2607_28069_amd as pic
-from page_path import DEV, SENTINEL, check, check_pages, decode, reference, rope_table, rows, setup, suffix
+from page_path import DEV, SENTINEL, check, contiguous, decode, reference, rope_table, rows, setup, suffix
 
 pytestmark = pytest.mark.gpu
 
@@ -48,6 +48,31 @@ def test_decode_dealt_ranges_with_padding(d, base):
     x = setup(8, 2, d, "bf16", 64, base, [1, 1, 1], slack=12000 - max(max(base), 0))
     decode(x, n_splits=8)
     check(x)
+
+
+@pytest.mark.parametrize("hq,hkv,d,n_splits,base", [
+    (32, 8, 128, 0, [700, 64, 3]), (28, 4, 128, 0, [5000]), (8, 8, 64, 3, [1000, 2049]), (40, 2, 128, 5, [300, 900]),
+    (8, 2, 128, 8, [9000, 500, 12000]), (8, 2, 64, 8, [9000, 9000]), (32, 8, 128, 1, [40] * 40)])
+@pytest.mark.parametrize("rope", [False, True])
+def test_decode_bits_of_the_contiguous_call(hq, hkv, d, n_splits, base, rope):
+    for P in (16, 64):
+        x = setup(hq, hkv, d, "bf16", P, base, [1] * len(base), L=2)
+        ck, cv, cap = contiguous(x)
+        r = rope_table(x) if rope else None
+        decode(x, n_splits=n_splits, rope=r)
+        ws = torch.empty(max(pic.pic_decode_workspace_bytes(x.model, x.B, x.max_ctx + 1, n_splits), 16), dtype=torch.uint8,
+                         device=DEV)
+        out = torch.empty_like(x.out)
+        args = (x.model, x.q, x.k, x.v, ck, cv, x.B, cap, x.len, 0, x.max_ctx)
+        if rope:
+            pic.pic_decode_attn_rope(*args, *r, out, ws, n_splits)
+        else:
+            pic.pic_decode_attn(*args, out, ws, n_splits)
+        assert (out == x.out).all()
+        for b in range(x.B):
+            r0 = rows(x, b, 0, base[b] + 1)
+            for p, c in ((x.pk, ck), (x.pv, cv)):
+                assert (p[:, :, r0] == c[:, b, :, : base[b] + 1]).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
