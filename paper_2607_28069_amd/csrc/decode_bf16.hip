@@ -298,9 +298,9 @@ decode_bf16_kernel(DecodeArgs a) {
   const int c1 = min(c0 + sub, wc1);
 
   const int64_t bh_kv = (((int64_t)l * a.batch + b) * a.n_kv_heads + g);
-  const int64_t row0 = kPages ? ((int64_t)l * a.n_kv_heads + g) * a.stream_rows : bh_kv * a.cache_cap;
-  const bf16_t* Kg = a.cache_k + row0 * kHD;
-  const bf16_t* Vg = a.cache_v + row0 * kHD;
+  const int64_t row0 = kPages ? ((int64_t)l * a.n_kv_heads + g) * a.stream_rows : 0;   // (pages) the stream's rows
+  const bf16_t* Kg = a.cache_k + (kPages ? row0 * kHD : bh_kv * a.cache_cap * kHD);
+  const bf16_t* Vg = a.cache_v + (kPages ? row0 * kHD : bh_kv * a.cache_cap * kHD);
   const bf16_t* Kn = a.k_new + bh_kv * kHD;
   const bf16_t* Vn = a.v_new + bh_kv * kHD;
 
@@ -366,7 +366,7 @@ decode_bf16_kernel(DecodeArgs a) {
   if constexpr (kPages) {   // (stored after the key loop: nothing there waits for the entry)
     if (stores) store_row = page_store_row(a.map, b, p);
   } else if (stores) {
-    store_new(row0 + p);
+    store_new(bh_kv * a.cache_cap + p);
   }
 
   const int n = lane & 15, g4 = lane >> 4;

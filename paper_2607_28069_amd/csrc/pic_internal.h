@@ -150,6 +150,8 @@ struct PageAttnArgs {
 hipError_t launch_page_attn(pic_dtype dt, const PageAttnArgs& a);
 // The decode of bf16 pages: n_new 1, no n_valid.
 hipError_t launch_decode_bf16_pages(const PageAttnArgs& a);
+// The prefill of bf16 pages: offset 0.
+hipError_t launch_prefill_bf16_pages(const PageAttnArgs& a);
 
 // Page pairs[i][1] = page pairs[i][0] in each of the n_streams (layer, kv head) streams of both
 // buffers; pages of page_bytes bytes, n_pages per stream.  `pairs` is host memory, read before the call returns.

@@ -395,8 +395,10 @@ pic_status page_attn(const pic_model* model, const pic_pages* pages, const void*
   a.ws_bytes = ws_bytes;
   a.n_splits = n_splits;
   a.stream = (hipStream_t)stream;
-  if (decode) return hip_status(model->dtype == PIC_BF16 ? launch_decode_bf16_pages(a) : launch_page_attn(model->dtype, a), "page decode launch");
-  return hip_status(launch_page_attn(model->dtype, a), "page suffix launch");
+  const hipError_t e = model->dtype == PIC_F32 ? launch_page_attn(model->dtype, a)
+                       : decode                ? launch_decode_bf16_pages(a)
+                                               : launch_prefill_bf16_pages(a);
+  return hip_status(e, decode ? "page decode launch" : "page suffix launch");
 }
 
 }  // namespace

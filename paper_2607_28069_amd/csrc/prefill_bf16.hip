@@ -160,7 +160,7 @@ struct PrefillArgs {
   bf16_t* cache_v;
   const int32_t* ctx_len;
   const int32_t* q_pos;     // table mode: [B][n_suffix]
-  const int32_t* n_valid;   // table mode: [B]
+  const int32_t* n_valid;   // table mode: [B]; pages modes: [B] or NULL
   int32_t max_pos;          // table mode: positions are clamped to [0, max_pos]
   bf16_t* out;
   int32_t max_ctx, n_suffix, batch, cache_cap, n_q_heads, n_kv_heads;
@@ -176,6 +176,8 @@ struct PrefillArgs {
   int32_t f32_partials;     // float32
   float2* ws_ml;            // [n_splits][rows_total] (reference max, row sum)
   float scale_log2;
+  PageMap map;              // pages modes: cache_k / cache_v are [L][Hkv][stream_rows][D]
+  int32_t stream_rows;
 };
 
 // Rope mode = suffix mode with the suffix queries and keys given unrotated: the kernel turns
@@ -183,7 +185,12 @@ struct PrefillArgs {
 // Runs mode = paged mode with a tile map whose non-run context tiles have been composed into
 // the cache beforehand: whole-run tiles come from the pool (queries turned), all others from
 // the cache, so the loop carries no per-key rotation.
-constexpr int kModeSuffix = 0, kModeTable = 1, kModePaged = 2, kModeRope = 3, kModeRuns = 4;
+// Pages modes = suffix and rope mode over a cache handed out in pages of at least 16 tokens, with
+// n_valid[b] of the n_suffix tokens used per request.  A load instruction moves 4 or 8 rows of a tile,
+// which lie in one page: a wave needs one page number per instruction, taken with readlane out of the
+// table's next 64 entries (the 64 after those on their way).
+constexpr int kModeSuffix = 0, kModeTable = 1, kModePaged = 2, kModeRope = 3, kModeRuns = 4, kModePages = 5,
+              kModePagesRope = 6;
 
 // (x, y) turned by the angle with cosine c and sine s, in the float32 arithmetic the compose
 // and re-rotation kernels use, so fused and separate rotations round identically.
@@ -222,7 +229,9 @@ __device__ __forceinline__ void rot_chunks(float (&x1)[8], float (&x2)[8], const
 template <int HD, int kMode, bool kInterleaved>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 prefill_bf16_kernel(PrefillArgs a) {
-  constexpr bool kTable = kMode == kModeTable, kPaged = kMode == kModePaged, kRope = kMode == kModeRope;
+  constexpr bool kTable = kMode == kModeTable, kPaged = kMode == kModePaged;
+  constexpr bool kPages = kMode == kModePages || kMode == kModePagesRope;
+  constexpr bool kRope = kMode == kModeRope || kMode == kModePagesRope;
   constexpr bool kRuns = kMode == kModeRuns, kPool = kPaged || kRuns;   // kPool: whole-run tiles from the pool
   static_assert(HD == 128 || HD == 64, "head dim");
   constexpr int kHD = HD;
@@ -271,7 +280,10 @@ prefill_bf16_kernel(PrefillArgs a) {
   // and with them every tile count, mask decision and load path derived from them)
   const int n_rep = a.n_rep;
   auto div_rep = [&](int x) { return (int)(((uint64_t)(uint32_t)x * a.rep_magic) >> 32); };
-  const int M = a.n_suffix * n_rep;
+  // tokens of this request (pages modes: the used ones)
+  const int n_tok = kPages ? page_new_tokens(a.ctx_len, a.n_valid, b, a.n_suffix) : a.n_suffix;
+  if (kPages && n_tok == 0) return;   // (uniform) padding of the batch
+  const int M = n_tok * n_rep;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // uniform: LDS bases in SGPRs
@@ -280,7 +292,7 @@ prefill_bf16_kernel(PrefillArgs a) {
   const int row0_wg = mt * kRowsPerWG;
   const int r = row0_wg + wave * kRowsPerWave + n;    // this lane's query row
   bool row_ok = r < M;
-  const int tok = row_ok ? div_rep(r) : a.n_suffix - 1;
+  const int tok = row_ok ? div_rep(r) : n_tok - 1;
   // ctx: keys below it come from the cache (suffix mode: the composed context);
   // pos_min_wg / pos_max_wg: nearest / furthest position of this workgroup's query rows
   int ctx, qpos, pos_min_wg, pos_max_wg, nv_wg = 0;   // nv_wg: table mode, the request's used tokens
@@ -318,7 +330,7 @@ prefill_bf16_kernel(PrefillArgs a) {
     qpos = row_ok ? p : pos_max_wg;
     ctx = pos_max_wg + 1;   // every visible key is in the cache
   }
-  const int n_keys = kTable ? pos_max_wg + 1 : ctx + a.n_suffix;
+  const int n_keys = kTable ? pos_max_wg + 1 : ctx + n_tok;
   // table mode: the wave's furthest query position.  A tile that starts past it holds no key
   // any of the wave's rows sees, so the wave skips the products and exponentials of every
   // tile from there on (it still moves its share of each tile and meets each barrier).  Rows
@@ -337,7 +349,8 @@ prefill_bf16_kernel(PrefillArgs a) {
   const int t0 = split * a.tiles_per_split;
   const int n_tiles = min((pos_max_wg + kKeys) / kKeys - t0, a.tiles_per_split);
 
-  const int64_t bh_kv = (((int64_t)l * a.batch + b) * a.n_kv_heads + g) * a.cache_cap;
+  const int64_t bh_kv = kPages ? ((int64_t)l * a.n_kv_heads + g) * a.stream_rows
+                               : (((int64_t)l * a.batch + b) * a.n_kv_heads + g) * a.cache_cap;
   const bf16_t* Kg = a.cache_k + bh_kv * kHD;
   const bf16_t* Vg = a.cache_v + bh_kv * kHD;
   // suffix token i of this (request, kv head): row i with a stride of Hkv rows
@@ -349,8 +362,33 @@ prefill_bf16_kernel(PrefillArgs a) {
   // (request, kv head)'s workgroups (every m-tile and split stores a contiguous share of the
   // rows), so no workgroup carries the whole store ahead of its key loop.
   const int asm_parts = a.m_tiles * a.n_splits, asm_part = split * a.m_tiles + mt;
-  const int asm_per = (a.n_suffix + asm_parts - 1) / asm_parts;
-  const int asm_i0 = min(asm_part * asm_per, a.n_suffix), asm_i1 = min(asm_i0 + asm_per, a.n_suffix);
+  const int asm_per = (n_tok + asm_parts - 1) / asm_parts;
+  const int asm_i0 = min(asm_part * asm_per, n_tok), asm_i1 = min(asm_i0 + asm_per, n_tok);
+  // pages: entries [pwin, pwin + 64) of the request's page table and the 64 after them, from this wave's
+  // first rows on
+  int32_t pwin = 0, w_cur = 0, w_next = 0;
+  auto entry = [&](int32_t i) { return a.map.table[(int64_t)b * a.map.cap + clamp_entry(i, a.map)]; };
+  if constexpr (kPages) {
+    pwin = (t0 * kKeys + kRowsPerLoad * wave) >> a.map.shift;
+    w_cur = entry(pwin + lane);
+    w_next = entry(pwin + 64 + lane);
+  }
+  // pages: the rows that this wave's load instructions of global tile T start at (T one more each time)
+  auto tile_rows = [&](int T, int32_t (&pr)[kLoadSteps]) {   // T uniform
+#pragma unroll
+    for (int i = 0; i < kLoadSteps; ++i) {
+      const int32_t slot = T * kKeys + kRowsPerLoad * (kWaves * i + wave), e = slot >> a.map.shift;
+      if (e >= pwin + 64) {
+        pwin += 64;
+        w_cur = w_next;
+        w_next = entry(pwin + 64 + lane);
+      }
+      const int32_t page = clamp_page(__builtin_amdgcn_readlane(w_cur, e - pwin), a.map);
+      pr[i] = (page << a.map.shift) + (slot & ((1 << a.map.shift) - 1));
+    }
+  };
+  // pages: the row of the stream where suffix token i is stored, or -1 (an entry that is no page)
+  auto store_row = [&](int i) { return (int32_t)page_store_row(a.map, b, ctx + i); };
   if (kRope) {   // with the suffix keys turned to ctx + i
     // item c: row i = c / (3 C / 2), C = D / 8 chunks; part < C / 2: K chunk pair part
     // (rotate-half: chunks part, part + C / 2; interleaved: 2 part, 2 part + 1; both:
@@ -362,11 +400,13 @@ prefill_bf16_kernel(PrefillArgs a) {
     for (int c0 = asm_i0 * kItems + tid; c0 < total; c0 += 3 * kThreads) {
       u32x4 w1[3], w2[3];
       float4 cs[3][4];
+      int32_t to[3];
 #pragma unroll
       for (int u = 0; u < 3; ++u) {
         const int c = c0 + u * kThreads;
         if (c >= total) continue;
         const int i = c / kItems, part = c - kItems * i;
+        if constexpr (kPages) to[u] = store_row(i);
         if (part < kHalfChunks) {
           const int o1 = kInterleaved ? 16 * part : 8 * part, o2 = kInterleaved ? 16 * part + 8 : kHD / 2 + 8 * part;
           w1[u] = *reinterpret_cast<const u32x4*>(Ks + i * suf_stride + o1);
@@ -383,6 +423,7 @@ prefill_bf16_kernel(PrefillArgs a) {
         const int c = c0 + u * kThreads;
         if (c >= total) continue;
         const int i = c / kItems, part = c - kItems * i;
+        if (kPages && to[u] < 0) continue;
         if (part < kHalfChunks) {
           const int o1 = kInterleaved ? 16 * part : 8 * part, o2 = kInterleaved ? 16 * part + 8 : kHD / 2 + 8 * part;
           float x1[8], x2[8];
@@ -398,11 +439,11 @@ prefill_bf16_kernel(PrefillArgs a) {
               rot_pair(x1[f], x2[f], cs2[f].x, cs2[f].y);
             }
           }
-          bf16_t* dst = a.cache_k + (bh_kv + ctx + i) * kHD;
+          bf16_t* dst = a.cache_k + (kPages ? bh_kv + to[u] : bh_kv + ctx + i) * kHD;
           *reinterpret_cast<u32x4*>(dst + o1) = pack8(x1);
           *reinterpret_cast<u32x4*>(dst + o2) = pack8(x2);
         } else {
-          *reinterpret_cast<u32x4*>(a.cache_v + (bh_kv + ctx + i) * kHD + 8 * (part - kHalfChunks)) = w1[u];
+          *reinterpret_cast<u32x4*>(a.cache_v + (kPages ? bh_kv + to[u] : bh_kv + ctx + i) * kHD + 8 * (part - kHalfChunks)) = w1[u];
         }
       }
     }
@@ -413,20 +454,23 @@ prefill_bf16_kernel(PrefillArgs a) {
     const int total = asm_i1 * 2 * kChunks;
     for (int c0 = asm_i0 * 2 * kChunks + tid; c0 < total; c0 += kU * kThreads) {
       u32x4 w[kU];
+      int32_t to[kU];
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
         const int c = c0 + u * kThreads, i = c >> kItemShift, part = c & (2 * kChunks - 1);
+        if constexpr (kPages) to[u] = c < total ? store_row(i) : -1;
         if (c < total)
           w[u] = *reinterpret_cast<const u32x4*>((part < kChunks ? Ks : Vs) + i * suf_stride + 8 * (part & (kChunks - 1)));
       }
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
         const int c = c0 + u * kThreads, i = c >> kItemShift, part = c & (2 * kChunks - 1);
-        if (c < total)
-          *reinterpret_cast<u32x4*>((part < kChunks ? a.cache_k : a.cache_v) + (bh_kv + ctx + i) * kHD + 8 * (part & (kChunks - 1))) = w[u];
+        if (kPages ? to[u] >= 0 : c < total)
+          *reinterpret_cast<u32x4*>((part < kChunks ? a.cache_k : a.cache_v) + (kPages ? bh_kv + to[u] : bh_kv + ctx + i) * kHD + 8 * (part & (kChunks - 1))) = w[u];
       }
     }
   }
+  if (kPages && row0_wg >= M) return;   // (uniform) no query row: stored its share of the suffix only
   // row of q / out / a split's partials of this request's packed row r2 (token r2 / n_rep)
   auto row_at = [&](int r2, int tok2) {
     return (((int64_t)l * a.batch + b) * a.n_suffix + tok2) * a.n_q_heads + g * n_rep + (r2 - tok2 * n_rep);
@@ -645,7 +689,8 @@ prefill_bf16_kernel(PrefillArgs a) {
   int32_t src_v[kLoadSteps], src_k[kLoadSteps], src_f[kLoadSteps];   // rows of tiles t+1, t+2, t+3
   int32_t d_k = 0, d_f = 0;                                            // rotation shift, tiles t+2, t+3
 
-  auto load_tile = [&](uint8_t* dst_tile, int t, bool is_v, int32_t run = -1) {
+  int32_t pr_cur[kLoadSteps] = {}, pr_next[kLoadSteps] = {};   // pages: rows (tile_rows) of tiles t + 1 and t + 2
+  auto load_tile = [&](uint8_t* dst_tile, int t, bool is_v, int32_t run = -1, const int32_t* pr = nullptr) {
     const uint32_t goff = 2u * (is_v ? v_goff : k_goff);   // bytes
     const uint32_t coff = 16u * (is_v ? v_gc : k_gc);
     const rsrc_t rc = is_v ? r_v : r_k, rs = is_v ? r_vs : r_ks;
@@ -664,6 +709,20 @@ prefill_bf16_kernel(PrefillArgs a) {
         // over the distinct bases)
         if (kk < ctx) dma16(is_v ? r_pv : r_pk, (uint32_t)rows[i] * kRowBytes + coff, 0, dst);
         if (kk >= ctx) dma16_other(rs, (uint32_t)((kk - ctx) * suf_stride) * 2u + coff, dst);
+      }
+    } else if constexpr (kPages) {
+      const uint32_t in_row = (uint32_t)(lane >> kChunkShift) * kRowBytes + coff;
+      const bool whole = (t + 1) * kKeys <= ctx;
+#pragma unroll
+      for (int i = 0; i < kLoadSteps; ++i) {
+        uint8_t* dst = dst_tile + (kRowsPerLoad * kWaves * i + kRowsPerLoad * wave) * kRowBytes;
+        if (whole) {
+          dma16(rc, in_row, (uint32_t)pr[i] * kRowBytes, dst);
+        } else {   // a tile reaching the suffix: its keys come from k_suf / v_suf
+          const int kk = min(t * kKeys + kRowsPerLoad * kWaves * i + ld_row, n_keys - 1);
+          if (kk < ctx) dma16(rc, in_row, (uint32_t)pr[i] * kRowBytes, dst);
+          if (kk >= ctx) dma16_other(rs, (uint32_t)((kk - ctx) * suf_stride) * 2u + coff, dst);
+        }
       }
     } else if ((t + 1) * kKeys <= ctx) {
 #pragma unroll
@@ -930,9 +989,11 @@ prefill_bf16_kernel(PrefillArgs a) {
     if (run_v >= 0 && del_v != 0 && del_v != q_shift) stage_row(del_v);
     wait_loads();
   } else {
-    load_tile(k_lds0, t0, false);
-    load_tile(v_lds0, t0, true);
-    if (n_tiles > 1) load_tile(k_lds1, t0 + 1, false);
+    if constexpr (kPages) tile_rows(t0, pr_next);
+    load_tile(k_lds0, t0, false, -1, pr_next);
+    load_tile(v_lds0, t0, true, -1, pr_next);
+    if constexpr (kPages) tile_rows(t0 + 1, pr_cur);
+    if (n_tiles > 1) load_tile(k_lds1, t0 + 1, false, -1, pr_cur);
     if constexpr (kRope) {
       if ((t0 + 1) * kKeys > ctx) rope_cs(t0);
       rope_q();
@@ -982,11 +1043,12 @@ prefill_bf16_kernel(PrefillArgs a) {
       if constexpr (!kIdle) turn_q(run_v >= 0 ? del_v : 0);
       if (t + 3 < n_tiles) run_f = tile_run(t0 + t + 3, del_f);
     }
+    if constexpr (kPages) tile_rows(t0 + t + 2, pr_next);
     // this tile's loads (K(t+2), V(t+1)): issued after the first slice outside paged mode,
     // so the waves' first LDS reads and products of the tile go ahead of them
     auto issue_loads = [&]() {
-      if (t + 2 < n_tiles) load_tile(k_free, t0 + t + 2, false, run_k);
-      if (t + 1 < n_tiles) load_tile(v_free, t0 + t + 1, true, run_v);
+      if (t + 2 < n_tiles) load_tile(k_free, t0 + t + 2, false, run_k, pr_next);
+      if (t + 1 < n_tiles) load_tile(v_free, t0 + t + 1, true, run_v, pr_cur);
     };
     if constexpr (kPaged || kIdle) issue_loads();
     if constexpr (kRope) {
@@ -1104,6 +1166,10 @@ prefill_bf16_kernel(PrefillArgs a) {
       run_k = run_f;
       del_k = del_f;
     }
+    if constexpr (kPages) {
+#pragma unroll
+      for (int i = 0; i < kLoadSteps; ++i) pr_cur[i] = pr_next[i];
+    }
     __syncthreads();
   };
 
@@ -1220,7 +1286,7 @@ prefill_bf16_kernel(PrefillArgs a) {
 // sum_s w_s O_s / sum_s w_s with w_s = 2^(m_s - M) l_s, M any common reference.  grid (rows_total / 16),
 // 2 D threads: D / 8 lanes per row, 8 head dims per lane; every split's loads are issued without a branch
 // between them (a split that saw no key of the row, reference max -inf, is dropped by a
-// select: its sums are not finite).  With n_valid (table mode), rows of tokens past
+// select: its sums are not finite).  With n_valid (table and pages modes), rows of tokens past
 // n_valid[b] are left untouched.
 // kBatch: splits whose loads are issued together (4, 8 or 16, the smallest that covers n_splits:
 // a larger batch holds more registers and lowers the occupancy that few splits need)
@@ -1230,6 +1296,7 @@ __global__ void __launch_bounds__(256) prefill_combine_kernel(const PT* __restri
                                                               const float2* __restrict__ ws_ml,
                                                               int32_t n_splits, int64_t rows_total,
                                                               const int32_t* __restrict__ n_valid,
+                                                              const int32_t* __restrict__ lens,
                                                               int32_t n_q, int32_t n_q_heads,
                                                               int32_t batch,
                                                               bf16_t* __restrict__ out) {
@@ -1237,11 +1304,12 @@ __global__ void __launch_bounds__(256) prefill_combine_kernel(const PT* __restri
   constexpr int kPieces = sizeof(PT) / 2;   // 16-byte pieces of a lane's 8 head dims
   const int64_t row = (int64_t)blockIdx.x * kCombineRowsPerWG + threadIdx.x / kLanes;
   if (row >= rows_total) return;
-  if (n_valid) {   // row = ((l * B + b) * n_q + i) * Hq + h
+  if (n_valid || lens) {   // row = ((l * B + b) * n_q + i) * Hq + h
     const int64_t ti = row / n_q_heads;
     const int i = (int)(ti % n_q);
     const int b = (int)((ti / n_q) % batch);
-    if (i >= n_valid[b]) return;
+    if (n_valid && i >= n_valid[b]) return;
+    if (lens && lens[b] < 0) return;   // pages modes: padding of the batch
   }
   const int d = 8 * (threadIdx.x & (kLanes - 1));
   // one pass with a running reference max, kCombineBatch splits at a time: all their loads
@@ -1455,16 +1523,24 @@ hipError_t launch_hd(const AttnShape& s, const PrefillArgs& a, const SplitPlan& 
     hipLaunchKernelGGL((prefill_bf16_kernel<HD, kModeRuns, false>), grid, dim3(kThreads), 0, stream, a);
   else if (mode == kModePaged)
     hipLaunchKernelGGL((prefill_bf16_kernel<HD, kModePaged, false>), grid, dim3(kThreads), 0, stream, a);
+  else if (mode == kModePagesRope && interleaved)
+    hipLaunchKernelGGL((prefill_bf16_kernel<HD, kModePagesRope, true>), grid, dim3(kThreads), 0, stream, a);
+  else if (mode == kModePagesRope)
+    hipLaunchKernelGGL((prefill_bf16_kernel<HD, kModePagesRope, false>), grid, dim3(kThreads), 0, stream, a);
+  else if (mode == kModePages)
+    hipLaunchKernelGGL((prefill_bf16_kernel<HD, kModePages, false>), grid, dim3(kThreads), 0, stream, a);
   else
     hipLaunchKernelGGL((prefill_bf16_kernel<HD, kModeSuffix, false>), grid, dim3(kThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_splits == 1) return e;
   const dim3 cgrid((unsigned)((a.rows_total + kCombineRowsPerWG - 1) / kCombineRowsPerWG));
   const dim3 cblock(kCombineRowsPerWG * HD / 8);
-  const int32_t* nv = mode == kModeTable ? a.n_valid : nullptr;
+  const bool pages = mode == kModePages || mode == kModePagesRope;
+  const int32_t* nv = mode == kModeTable || pages ? a.n_valid : nullptr;
+  const int32_t* lens = pages ? a.ctx_len : nullptr;
   auto combine = [&](auto* ws_o, auto batch) {
     hipLaunchKernelGGL((prefill_combine_kernel<HD, decltype(batch)::value, std::remove_pointer_t<decltype(ws_o)>>), cgrid,
-                       cblock, 0, stream, ws_o, a.ws_ml, p.n_splits, a.rows_total, nv, n_q, s.n_q_heads, s.batch, a.out);
+                       cblock, 0, stream, ws_o, a.ws_ml, p.n_splits, a.rows_total, nv, lens, n_q, s.n_q_heads, s.batch, a.out);
   };
   auto combine_as = [&](auto* ws_o) {
     if (p.n_splits <= 4) combine(ws_o, std::integral_constant<int, 4>{});
@@ -1657,6 +1733,26 @@ hipError_t launch_prefill_bf16_paged(const AttnShape& s, bool interleaved, const
     if (e != hipSuccess) return e;
   }
   return launch(s, a, kModeRuns, interleaved, n_suffix, max_ctx, workspace, ws_bytes, stream);
+}
+
+hipError_t launch_prefill_bf16_pages(const PageAttnArgs& p) {
+  PrefillArgs a = {};
+  a.q = static_cast<const bf16_t*>(p.q);
+  a.k_suf = static_cast<const bf16_t*>(p.k_new);
+  a.v_suf = static_cast<const bf16_t*>(p.v_new);
+  a.cache_k = static_cast<bf16_t*>(p.pages_k);
+  a.cache_v = static_cast<bf16_t*>(p.pages_v);
+  a.ctx_len = p.base_len;
+  a.n_valid = p.n_valid;
+  a.out = static_cast<bf16_t*>(p.out);
+  a.max_ctx = p.max_base;
+  a.table = p.table;
+  a.table_stride = p.table_stride;
+  a.max_abs_delta = p.max_abs_delta;
+  a.map = p.map;
+  a.stream_rows = p.s.cache_cap;
+  return launch(p.s, a, p.table ? kModePagesRope : kModePages, p.interleaved, p.n_new, p.max_base, p.workspace, p.ws_bytes,
+                p.stream);
 }
 
 }  // namespace pic

@@ -101,6 +101,30 @@ def test_suffix_lengths(dtype, n, ctx, P):
     check(x)
 
 
+@pytest.mark.parametrize("hq,hkv,d,n,ctx", [
+    (32, 8, 128, 70, [700, 64, 3]), (28, 4, 128, 128, [5000]), (8, 8, 64, 33, [1000, 2049, 0]), (40, 2, 128, 16, [300, 900]),
+    (8, 2, 64, 200, [4000]), (32, 8, 128, 128, [190] * 12), (4, 1, 128, 1, [6000, 77])])
+@pytest.mark.parametrize("rope", [False, True])
+def test_suffix_bits_of_the_contiguous_call(hq, hkv, d, n, ctx, rope):
+    for P in (16, 64, 512):
+        x = setup(hq, hkv, d, "bf16", P, ctx, [n] * len(ctx), L=2)
+        ck, cv, cap = contiguous(x)
+        r = rope_table(x) if rope else None
+        suffix(x, rope=r, n_valid=None if P == 64 else "given")
+        ws = torch.empty(max(pic.pic_prefill_workspace_bytes(x.model, x.B, n, x.max_ctx), 16), dtype=torch.uint8, device=DEV)
+        out = torch.empty_like(x.out)
+        args = (x.model, x.q, x.k, x.v, ck, cv, x.B, cap, x.len, x.max_ctx, n)
+        if rope:
+            pic.pic_suffix_prefill_attn_rope(*args, *r, out, ws)
+        else:
+            pic.pic_suffix_prefill_attn(*args, out, ws)
+        assert (out == x.out).all()
+        for b in range(x.B):
+            r0 = rows(x, b, 0, ctx[b] + n)
+            for p, c in ((x.pk, ck), (x.pv, cv)):
+                assert (p[:, :, r0] == c[:, b, :, : ctx[b] + n]).all()
+
+
 def test_suffix_all_padding():
     for dtype in ("bf16", "f32"):
         x = setup(4, 2, 64, dtype, 16, [-1, 50, 0], [9, 0, 0], n=9)
