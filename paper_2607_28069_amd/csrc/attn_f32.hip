@@ -30,6 +30,9 @@
 //  * A tile some rows see only in part has its scores masked; a probability of 0 times a value
 //    that is not finite is no 0, so a tile that holds such a value takes its PV products one
 //    query column at a time, with the values that column does not see cleared.
+//  * A paged cache: a 16-key tile lies in one page (pages hold 16 tokens or more), so a tile costs one
+//    page number, taken with readlane out of the table's next 64 entries, which a wave holds in a
+//    register (the 64 after those on their way).
 #include <algorithm>
 
 #include "pic_bounds.h"
@@ -47,6 +50,13 @@ __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
+// A paged cache: cache_k / cache_v are [L][Hkv][s.cache_cap][D], and token i of request b is used for
+// i < page_new_tokens(pos.base, n_valid, b, n_q).
+struct F32Pages {
+  PageMap map;
+  const int32_t* n_valid = nullptr;
+};
+
 // Lanes n, n + 16, n + 32, n + 48 hold the same query column.
 __device__ __forceinline__ float column_max(float x) {
   auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -63,8 +73,9 @@ __device__ __forceinline__ float column_sum(float x) {
 
 // grid (ceil(n_units / 8) * 8, L), 64 W threads; NB blocks of 16 query rows.  Units [unit0, unit0 +
 // n_units) of the m_tiles * batch * Hkv.
-template <int HD, int NB, int W>
-__global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t m_tiles, int32_t unit0, int32_t n_units) {
+template <int HD, int NB, int W, bool kPages>
+__global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t m_tiles, int32_t unit0, int32_t n_units,
+                                                       F32Pages pg) {
   constexpr int QJ = HD / 16;         // 16-byte pieces of a Q or K row per lane
   constexpr int VH = HD / 64;         // 16-byte pieces of a V row per lane
   constexpr int ROWS = 16 * NB;
@@ -86,6 +97,28 @@ __global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int M = n_q * n_rep, row0 = mt * ROWS;
+  // pages: the used tokens of this request (uniform)
+  const int n_tok = kPages ? page_new_tokens(a.pos.base, pg.n_valid, b, n_q) : n_q;
+  if (kPages && n_tok == 0) return;   // padding of the batch
+  auto pos_of = [&](int tok) -> int64_t { return kPages && tok >= n_tok ? -1 : a.pos(b, tok); };
+  int32_t win = 0, w_cur = 0, w_next = 0;   // entries [win, win + 64) of the page table, and the 64 after them
+  auto entry = [&](int32_t i) { return pg.map.table[(int64_t)b * pg.map.cap + clamp_entry(i, pg.map)]; };
+  if constexpr (kPages) {
+    win = (wave * kTile) >> pg.map.shift;
+    w_cur = entry(win + lane);
+    w_next = entry(win + 64 + lane);
+  }
+  // pages: the row of the stream where tile t starts (t uniform, never less than the one asked for before)
+  auto tile_row = [&](int t) -> int64_t {
+    const int32_t e = (t * kTile) >> pg.map.shift;
+    if (e >= win + 64) {
+      win += 64;
+      w_cur = w_next;
+      w_next = entry(win + 64 + lane);
+    }
+    const int32_t page = clamp_page(__builtin_amdgcn_readlane(w_cur, e - win), pg.map);
+    return ((int64_t)page << pg.map.shift) + ((t * kTile) & ((1 << pg.map.shift) - 1));
+  };
 
   // query rows and their positions; an unused row (past M, or a token without a position) takes
   // the workgroup's furthest position and is dropped at the end
@@ -96,7 +129,7 @@ __global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t
   for (int nb = 0; nb < NB; ++nb) {
     const int r = row0 + 16 * nb + n;
     const int tok = r < M ? r / n_rep : n_q - 1;
-    const int64_t p = a.pos(b, tok);
+    const int64_t p = pos_of(tok);
     row_ok[nb] = r < M && p >= 0;
     qpos[nb] = (int)p;
     qrow[nb] = (lb * n_q + tok) * Hq + g * n_rep + (r < M ? r - tok * n_rep : 0);
@@ -114,19 +147,21 @@ __global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t
   // slots from `fresh` on are the call's own tokens (table positions: all slots are in the cache)
   const int fresh = a.k_new ? (int)a.pos(b, 0) : INT32_MAX;
 
-  const int64_t kv0 = (lb * Hkv + g) * s.cache_cap * HD;
+  const int64_t kv0 = (kPages ? (int64_t)l * Hkv + g : lb * Hkv + g) * s.cache_cap * HD;
   const float* Kg = a.cache_k + kv0;
   const float* Vg = a.cache_v + kv0;
   const int64_t new0 = (lb * n_q * Hkv + g) * HD;
   const int64_t new_stride = (int64_t)Hkv * HD;
   if (a.k_new) {   // this workgroup's share of the new rows -> the cache, 16 bytes per thread
     constexpr int CPR = HD / 4;
-    const int per = (n_q + m_tiles - 1) / m_tiles;
-    const int i0 = min(mt * per, n_q), i1 = min(i0 + per, n_q);
+    const int per = (n_tok + m_tiles - 1) / m_tiles;
+    const int i0 = min(mt * per, n_tok), i1 = min(i0 + per, n_tok);
     for (int c = tid; c < (i1 - i0) * 2 * CPR; c += 64 * W) {
       const int i = i0 + c / (2 * CPR), part = c % (2 * CPR), d = 4 * (part % CPR);
       const float* src = (part < CPR ? a.k_new : a.v_new) + new0 + i * new_stride + d;
-      float* dst = (part < CPR ? a.cache_k : a.cache_v) + kv0 + (int64_t)(fresh + i) * HD + d;
+      const int64_t to = kPages ? page_store_row(pg.map, b, fresh + i) : fresh + i;
+      if (kPages && to < 0) continue;
+      float* dst = (part < CPR ? a.cache_k : a.cache_v) + kv0 + to * HD + d;
       *reinterpret_cast<f32x4*>(dst) = *reinterpret_cast<const f32x4*>(src);
     }
   }
@@ -212,8 +247,9 @@ __global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t
   {
     const int k_lane = n * HD + 4 * g4, v_lane = 4 * g4 * HD + 4 * n;
     auto load = [&](int t, f32x4 (&kr)[QJ], f32x4 (&vr)[4][VH]) {
-      const float* kp = Kg + (int64_t)t * (kTile * HD);
-      const float* vp = Vg + (int64_t)t * (kTile * HD);
+      const int64_t at = kPages ? tile_row(t) * HD : (int64_t)t * (kTile * HD);
+      const float* kp = Kg + at;
+      const float* vp = Vg + at;
 #pragma unroll
       for (int j = 0; j < QJ; ++j) kr[j] = *reinterpret_cast<const f32x4*>(kp + k_lane + 16 * j);
 #pragma unroll
@@ -247,9 +283,10 @@ __global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t
   // are masked, their values cleared).
   for (; t < n_tiles; t += W) {
     const int k0 = t * kTile;
+    const int64_t at = kPages ? tile_row(t) - k0 : 0;
     auto row_of = [&](const float* cache, const float* fresh_rows, int key) {
       key = min(key, last);
-      return key < fresh ? cache + (int64_t)key * HD : fresh_rows + new0 + (int64_t)(key - fresh) * new_stride;
+      return key < fresh ? cache + (at + key) * HD : fresh_rows + new0 + (int64_t)(key - fresh) * new_stride;
     };
     f32x4 kr[QJ], vr[4][VH], p[NB];
     const float* kp = row_of(Kg, a.k_new, k0 + n) + 4 * g4;
@@ -321,7 +358,7 @@ __global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t
     const int r = row0 + rr;
     if (r >= M) continue;
     const int tok = r / n_rep;
-    if (a.pos(b, tok) < 0) continue;   // a token without a position: its row is left untouched
+    if (pos_of(tok) < 0) continue;   // a token without a position: its row is left untouched
     float m = -INFINITY;
 #pragma unroll
     for (int w = 0; w < W; ++w) m = fmaxf(m, m_lds[w * ROWS + rr]);
@@ -339,8 +376,8 @@ __global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t
   }
 }
 
-template <int HD, int NB, int W>
-hipError_t launch_as(const F32AttnArgs& a) {
+template <int HD, int NB, int W, bool kPages>
+hipError_t launch_as(const F32AttnArgs& a, const F32Pages& pg) {
   const int64_t M = (int64_t)a.n_q * (a.s.n_q_heads / a.s.n_kv_heads);
   const int64_t m_tiles = (M + 16 * NB - 1) / (16 * NB);
   const int64_t units = m_tiles * a.s.batch * a.s.n_kv_heads;   // at most the query rows: fits int32
@@ -348,17 +385,16 @@ hipError_t launch_as(const F32AttnArgs& a) {
   constexpr int64_t kPart = int64_t(1) << 22;
   for (int64_t u0 = 0; u0 < units; u0 += kPart) {
     const int64_t part = std::min(units - u0, kPart), grid = (part + kNumXcd - 1) / kNumXcd * kNumXcd;
-    hipLaunchKernelGGL((attn_f32_kernel<HD, NB, W>), dim3((unsigned)grid, a.s.n_layers), dim3(64 * W), 0, a.stream, a,
-                       (int32_t)m_tiles, (int32_t)u0, (int32_t)part);
+    hipLaunchKernelGGL((attn_f32_kernel<HD, NB, W, kPages>), dim3((unsigned)grid, a.s.n_layers), dim3(64 * W), 0, a.stream, a,
+                       (int32_t)m_tiles, (int32_t)u0, (int32_t)part, pg);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-}  // namespace
-
-hipError_t launch_attn_f32(const F32AttnArgs& a) {
+template <bool kPages>
+hipError_t launch_shape(const F32AttnArgs& a, const F32Pages& pg) {
   const int64_t M = (int64_t)a.n_q * (a.s.n_q_heads / a.s.n_kv_heads);
   const int64_t pairs = (int64_t)a.s.batch * a.s.n_kv_heads * a.s.n_layers;
   if (M == 0 || pairs == 0) return hipSuccess;
@@ -369,9 +405,33 @@ hipError_t launch_attn_f32(const F32AttnArgs& a) {
   // Eight waves: sixteen took 29.3 us instead of 26.3.  Head_dim 128 with 32 rows needs the
   // registers of one wave per SIMD: eight waves took 212 us instead of 148.
   const bool wide = M > 16 && (M + 31) / 32 * pairs >= 256;
-  if (a.s.head_dim == 64) return wide ? launch_as<64, 2, 8>(a) : launch_as<64, 1, 8>(a);
-  if (a.s.head_dim == 128) return wide ? launch_as<128, 2, 4>(a) : launch_as<128, 1, 8>(a);
+  if (a.s.head_dim == 64) return wide ? launch_as<64, 2, 8, kPages>(a, pg) : launch_as<64, 1, 8, kPages>(a, pg);
+  if (a.s.head_dim == 128) return wide ? launch_as<128, 2, 4, kPages>(a, pg) : launch_as<128, 1, 8, kPages>(a, pg);
   return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_attn_f32(const F32AttnArgs& a) { return launch_shape<false>(a, F32Pages()); }
+
+hipError_t launch_attn_f32_pages(const PageAttnArgs& p) {
+  F32AttnArgs a;
+  a.s = p.s;
+  a.q = static_cast<const float*>(p.q);
+  a.k_new = static_cast<const float*>(p.k_new);
+  a.v_new = static_cast<const float*>(p.v_new);
+  a.cache_k = static_cast<float*>(p.pages_k);
+  a.cache_v = static_cast<float*>(p.pages_v);
+  a.pos.base = p.base_len;
+  a.pos.max_base = p.max_base;
+  a.pos.offset = p.offset;
+  a.n_q = p.n_new;
+  a.out = static_cast<float*>(p.out);
+  a.stream = p.stream;
+  F32Pages pg;
+  pg.map = p.map;
+  pg.n_valid = p.n_valid;
+  return launch_shape<true>(a, pg);
 }
 
 }  // namespace pic

@@ -147,7 +147,8 @@ struct PageAttnArgs {
   int32_t n_splits = 0;
   hipStream_t stream = nullptr;
 };
-hipError_t launch_page_attn(pic_dtype dt, const PageAttnArgs& a);
+// Float32 pages.
+hipError_t launch_attn_f32_pages(const PageAttnArgs& a);
 // The decode of bf16 pages: n_new 1, no n_valid.
 hipError_t launch_decode_bf16_pages(const PageAttnArgs& a);
 // The prefill of bf16 pages: offset 0.

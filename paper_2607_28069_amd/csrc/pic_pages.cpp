@@ -395,7 +395,7 @@ pic_status page_attn(const pic_model* model, const pic_pages* pages, const void*
   a.ws_bytes = ws_bytes;
   a.n_splits = n_splits;
   a.stream = (hipStream_t)stream;
-  const hipError_t e = model->dtype == PIC_F32 ? launch_page_attn(model->dtype, a)
+  const hipError_t e = model->dtype == PIC_F32 ? launch_attn_f32_pages(a)
                        : decode                ? launch_decode_bf16_pages(a)
                                                : launch_prefill_bf16_pages(a);
   return hip_status(e, decode ? "page decode launch" : "page suffix launch");

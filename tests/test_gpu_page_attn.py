@@ -125,6 +125,22 @@ def test_suffix_bits_of_the_contiguous_call(hq, hkv, d, n, ctx, rope):
                 assert (p[:, :, r0] == c[:, b, :, : ctx[b] + n]).all()
 
 
+@pytest.mark.parametrize("hq,hkv,d,n,ctx", [(4, 2, 64, 1, [289]), (16, 4, 64, 61, [500, 333]), (32, 8, 128, 64, [700] * 8),
+                                            (8, 8, 128, 1, [3000, 0, 17]), (32, 2, 64, 100, [200] * 20)])
+def test_f32_bits_of_the_contiguous_call(hq, hkv, d, n, ctx):
+    for P in (16, 128):
+        x = setup(hq, hkv, d, "f32", P, ctx, [n] * len(ctx), L=2)
+        ck, cv, cap = contiguous(x)
+        out = torch.empty_like(x.out)
+        if n == 1:
+            decode(x)
+            pic.pic_decode_attn(x.model, x.q, x.k, x.v, ck, cv, x.B, cap, x.len, 0, x.max_ctx, out)
+        else:
+            suffix(x)
+            pic.pic_suffix_prefill_attn(x.model, x.q, x.k, x.v, ck, cv, x.B, cap, x.len, x.max_ctx, n, out)
+        assert (out == x.out).all()
+
+
 def test_suffix_all_padding():
     for dtype in ("bf16", "f32"):
         x = setup(4, 2, 64, dtype, 16, [-1, 50, 0], [9, 0, 0], n=9)
