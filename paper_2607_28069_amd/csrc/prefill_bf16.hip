@@ -364,27 +364,32 @@ prefill_bf16_kernel(PrefillArgs a) {
   const int asm_parts = a.m_tiles * a.n_splits, asm_part = split * a.m_tiles + mt;
   const int asm_per = (n_tok + asm_parts - 1) / asm_parts;
   const int asm_i0 = min(asm_part * asm_per, n_tok), asm_i1 = min(asm_i0 + asm_per, n_tok);
-  // pages: entries [pwin, pwin + 64) of the request's page table and the 64 after them, from this wave's
-  // first rows on
-  int32_t pwin = 0, w_cur = 0, w_next = 0;
+  // pages: lane j holds where page table entry pwin + j lies in a stream, in bytes, and entry pwin + 56 + j
+  // as the table gives it (a tile's rows lie in 4 pages at most, so a window can move on by 56 before
+  // its last entries are needed); from this wave's first rows on
+  constexpr int kWindow = 56;
+  int32_t pwin = 0, w_next = 0;
+  uint32_t w_cur = 0;
   auto entry = [&](int32_t i) { return a.map.table[(int64_t)b * a.map.cap + clamp_entry(i, a.map)]; };
+  auto page_bytes = [&](int32_t page) { return ((uint32_t)clamp_page(page, a.map) << a.map.shift) * kRowBytes; };
   if constexpr (kPages) {
     pwin = (t0 * kKeys + kRowsPerLoad * wave) >> a.map.shift;
-    w_cur = entry(pwin + lane);
-    w_next = entry(pwin + 64 + lane);
+    w_next = entry(pwin + kWindow + lane);
+    w_cur = page_bytes(entry(pwin + lane));
   }
-  // pages: the rows that this wave's load instructions of global tile T start at (T one more each time)
-  auto tile_rows = [&](int T, int32_t (&pr)[kLoadSteps]) {   // T uniform
+  // pages: where the rows that this wave's load instructions of global tile T move lie, in bytes (T one
+  // more each time)
+  auto tile_rows = [&](int T, uint32_t (&pr)[kLoadSteps]) {   // T uniform
+    if (((T * kKeys + kRowsPerLoad * wave) >> a.map.shift) >= pwin + kWindow) {
+      pwin += kWindow;
+      w_cur = page_bytes(w_next);
+      w_next = entry(pwin + kWindow + lane);
+    }
 #pragma unroll
     for (int i = 0; i < kLoadSteps; ++i) {
-      const int32_t slot = T * kKeys + kRowsPerLoad * (kWaves * i + wave), e = slot >> a.map.shift;
-      if (e >= pwin + 64) {
-        pwin += 64;
-        w_cur = w_next;
-        w_next = entry(pwin + 64 + lane);
-      }
-      const int32_t page = clamp_page(__builtin_amdgcn_readlane(w_cur, e - pwin), a.map);
-      pr[i] = (page << a.map.shift) + (slot & ((1 << a.map.shift) - 1));
+      const int32_t slot = T * kKeys + kRowsPerLoad * (kWaves * i + wave);
+      const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)w_cur, (slot >> a.map.shift) - pwin);
+      pr[i] = at + (uint32_t)(slot & ((1 << a.map.shift) - 1)) * kRowBytes;
     }
   };
   // pages: the row of the stream where suffix token i is stored, or -1 (an entry that is no page)
@@ -689,8 +694,8 @@ prefill_bf16_kernel(PrefillArgs a) {
   int32_t src_v[kLoadSteps], src_k[kLoadSteps], src_f[kLoadSteps];   // rows of tiles t+1, t+2, t+3
   int32_t d_k = 0, d_f = 0;                                            // rotation shift, tiles t+2, t+3
 
-  int32_t pr_cur[kLoadSteps] = {}, pr_next[kLoadSteps] = {};   // pages: rows (tile_rows) of tiles t + 1 and t + 2
-  auto load_tile = [&](uint8_t* dst_tile, int t, bool is_v, int32_t run = -1, const int32_t* pr = nullptr) {
+  uint32_t pr_cur[kLoadSteps] = {}, pr_next[kLoadSteps] = {};   // pages: tile_rows of tiles t + 1 and t + 2
+  auto load_tile = [&](uint8_t* dst_tile, int t, bool is_v, int32_t run = -1, const uint32_t* pr = nullptr) {
     const uint32_t goff = 2u * (is_v ? v_goff : k_goff);   // bytes
     const uint32_t coff = 16u * (is_v ? v_gc : k_gc);
     const rsrc_t rc = is_v ? r_v : r_k, rs = is_v ? r_vs : r_ks;
@@ -712,15 +717,16 @@ prefill_bf16_kernel(PrefillArgs a) {
       }
     } else if constexpr (kPages) {
       const uint32_t in_row = (uint32_t)(lane >> kChunkShift) * kRowBytes + coff;
-      const bool whole = (t + 1) * kKeys <= ctx;
+      if ((t + 1) * kKeys <= ctx) {
 #pragma unroll
-      for (int i = 0; i < kLoadSteps; ++i) {
-        uint8_t* dst = dst_tile + (kRowsPerLoad * kWaves * i + kRowsPerLoad * wave) * kRowBytes;
-        if (whole) {
-          dma16(rc, in_row, (uint32_t)pr[i] * kRowBytes, dst);
-        } else {   // a tile reaching the suffix: its keys come from k_suf / v_suf
+        for (int i = 0; i < kLoadSteps; ++i)
+          dma16(rc, in_row, pr[i], dst_tile + (kRowsPerLoad * kWaves * i + kRowsPerLoad * wave) * kRowBytes);
+      } else {   // a tile reaching the suffix: its keys come from k_suf / v_suf
+#pragma unroll
+        for (int i = 0; i < kLoadSteps; ++i) {
           const int kk = min(t * kKeys + kRowsPerLoad * kWaves * i + ld_row, n_keys - 1);
-          if (kk < ctx) dma16(rc, in_row, (uint32_t)pr[i] * kRowBytes, dst);
+          uint8_t* dst = dst_tile + (kRowsPerLoad * kWaves * i + kRowsPerLoad * wave) * kRowBytes;
+          if (kk < ctx) dma16(rc, in_row, pr[i], dst);
           if (kk >= ctx) dma16_other(rs, (uint32_t)((kk - ctx) * suf_stride) * 2u + coff, dst);
         }
       }
@@ -994,6 +1000,7 @@ prefill_bf16_kernel(PrefillArgs a) {
     load_tile(v_lds0, t0, true, -1, pr_next);
     if constexpr (kPages) tile_rows(t0 + 1, pr_cur);
     if (n_tiles > 1) load_tile(k_lds1, t0 + 1, false, -1, pr_cur);
+    if constexpr (kPages) tile_rows(t0 + 2, pr_next);
     if constexpr (kRope) {
       if ((t0 + 1) * kKeys > ctx) rope_cs(t0);
       rope_q();
@@ -1043,14 +1050,21 @@ prefill_bf16_kernel(PrefillArgs a) {
       if constexpr (!kIdle) turn_q(run_v >= 0 ? del_v : 0);
       if (t + 3 < n_tiles) run_f = tile_run(t0 + t + 3, del_f);
     }
-    if constexpr (kPages) tile_rows(t0 + t + 2, pr_next);
     // this tile's loads (K(t+2), V(t+1)): issued after the first slice outside paged mode,
     // so the waves' first LDS reads and products of the tile go ahead of them
     auto issue_loads = [&]() {
       if (t + 2 < n_tiles) load_tile(k_free, t0 + t + 2, false, run_k, pr_next);
       if (t + 1 < n_tiles) load_tile(v_free, t0 + t + 1, true, run_v, pr_cur);
     };
+    // pages: the rows of the next tile's loads, once this tile's are on their way (between its products:
+    // before the barrier or at the tile's start they cost 2 %)
+    auto next_rows = [&]() {
+#pragma unroll
+      for (int i = 0; i < kLoadSteps; ++i) pr_cur[i] = pr_next[i];
+      tile_rows(t0 + t + 3, pr_next);
+    };
     if constexpr (kPaged || kIdle) issue_loads();
+    if constexpr (kPages && kIdle) next_rows();
     if constexpr (kRope) {
       if (t + 2 < n_tiles && (t0 + t + 3) * kKeys > ctx) rope_cs(t0 + t + 2);
     }
@@ -1139,6 +1153,7 @@ prefill_bf16_kernel(PrefillArgs a) {
       }
       if constexpr (!kPaged) {
         if (s4 == 0) issue_loads();
+        if (kPages && s4 == 1) next_rows();
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -1165,10 +1180,6 @@ prefill_bf16_kernel(PrefillArgs a) {
       del_v = del_k;
       run_k = run_f;
       del_k = del_f;
-    }
-    if constexpr (kPages) {
-#pragma unroll
-      for (int i = 0; i < kLoadSteps; ++i) pr_cur[i] = pr_next[i];
     }
     __syncthreads();
   };
