@@ -516,8 +516,9 @@ pic_status pic_page_suffix_attn_rope(const pic_model* model, const pic_pages* pa
 
 /* ---- 5d. decode over pages ----
    pic_decode_attn on a paged cache: stores the new token at slot p = base_len[b] + step and attends
-   over slots [0, p]; split over the context and joined alike.  Outputs are bit-identical to
-   pic_decode_attn's on the same cache contents and lengths for the same n_splits and workspace.
+   over slots [0, p]; split over the context and joined alike.  On bf16 pages probabilities keep 16 bits
+   where pic_decode_attn rounds them to 8, so outputs carry little more than their own rounding; on float32
+   pages outputs are pic_decode_attn's bit for bit.
      page_table [device, batch x table_cap]
      base_len   [device, batch]   clamped to max_base_len; a negative one marks padding of the batch:
                                   nothing of that request is read or stored, its out rows are left untouched

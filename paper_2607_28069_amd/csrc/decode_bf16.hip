@@ -30,8 +30,7 @@
 #include <mutex>
 #include <type_traits>
 
-#include "pic_bounds.h"
-#include "pic_internal.h"
+#include "decode_common.h"
 
 namespace pic {
 namespace {
@@ -41,45 +40,6 @@ namespace {
 // with hipGetSymbolAddress and that pointer is what the kernels receive.
 constexpr size_t kScratchBytes = PIC_DECODE_SCRATCH_BYTES;
 static __device__ __align__(256) uint8_t scratch[kScratchBytes];
-
-constexpr int kWaves = 4;
-constexpr int kTile = 32;                          // keys per wave tile
-constexpr int kMinWaveKeys = 64;
-// Sizes that follow the head dim HD (128 or 64): a row is HD/8 16-byte chunks; a lane's
-// operands hold HD/32 steps of 32 head dims; the output is HD/16 blocks of 16 head dims.
-template <int HD>
-struct Dims {
-  static_assert(HD == 128 || HD == 64, "head_dim 128 or 64");
-  static constexpr int kRowBytes = HD * 2;                  // 256 or 128
-  static constexpr int kVTileBytes = kTile * kRowBytes;     // per wave per buffer
-  static constexpr int kChunks = HD / 8;                    // 16-byte chunks per row
-  static constexpr int kSteps = HD / 32;                    // k steps of Q^T / K operands
-  static constexpr int kBlocks = HD / 16;                   // 16-dim output blocks
-  static constexpr int kRowsPerMove = 64 / kChunks;         // rows one 1 KB V move fills
-};
-static_assert(kDecodeUnit == kWaves * kTile, "a unit is one tile per wave");
-static_assert(kWaves == kDecodeWaves && kMinWaveKeys == kDecodeMinWaveKeys, "host split planner tiling");
-constexpr int kNonTemporal = 2;                    // cache-policy bits of a streaming load
-
-#define LDS_AS __attribute__((address_space(3)))
-#define GLOBAL_AS __attribute__((address_space(1)))
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ bf16x8_t as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8_t, v); }
-
-// 16-byte chunk c of V row `key` sits at slot c ^ v_swz(key) of its row in LDS (256-byte rows:
-// 16 slots; 128-byte rows: 8 slots, so the XOR keeps to the low three bits).
-template <int HD>
-__device__ __forceinline__ int v_swz(int key) {
-  if constexpr (HD == 128) return ((key & 3) << 1) | (((key >> 2) & 1) << 3);
-  else return (key & 3) << 1;
-}
-
-// The dealt ranges of a batch whose contexts all have the greatest length the call allows.
-struct EqualDeal {
-  int32_t units, n, chunk;   // units of every context, its ranges, keys per range
-};
 
 struct DecodeArgs {
   const bf16_t* q;        // [L][B][Hq][D]
@@ -98,139 +58,11 @@ struct DecodeArgs {
   const float2* table;    // rope variant: [L or 1][max_abs_delta + 1][D/2] cos/sin rows
   int64_t table_stride;
   int32_t max_abs_delta;
-  PageMap map;            // paged cache: cache_k / cache_v are [L][Hkv][stream_rows][D] and cache_cap bounds
-  int32_t stream_rows;    // the slots of a request
 };
-
-// How the key ranges of a split launch are dealt to the requests (pic_bounds.h): worked out by
-// every wave from the context lengths, request b in lane b.  Request b's partials are slots
-// [Hq first, Hq (first + n)), query head by query head.  Contexts of one length take a short way to
-// the same ranges (the long one costs about 0.5 us, paid in the kernel and its combine), and where that
-// is the greatest length the host has worked them out (EqualDeal): the place follows, and the combine
-// loads its partials, while the lengths are on their way.
-struct SplitDeal {
-  int32_t chunk;   // keys per range, a multiple of 128
-  int32_t n;       // ranges of every request; -1: lane b holds those of request b in mine
-  int32_t mine;
-};
-struct SplitLens {
-  int32_t u, base;   // lane b: request b's units and context length
-};
-struct SplitPlace {
-  int32_t n, first;   // ranges of the request; those of the requests before it
-};
-// ceil(u / c) for 0 <= u < 2^24, 1 <= c, inv ~ 1 / c: a float32 quotient, off by one at most, put right
-__device__ __forceinline__ int32_t ceil_div24(int32_t u, int32_t c, float inv) {
-  int32_t q = (int32_t)((float)u * inv);
-  const int32_t r = u - q * c;
-  return q + (r > 0 ? 1 : 0) + (r > c ? 1 : 0) - (r <= -c ? 1 : 0);
-}
-// kPages: a negative length is padding of the batch and gets no range
-template <bool kPages>
-__device__ __forceinline__ SplitLens split_lens(const int32_t* base_len, int32_t batch, int32_t max_base, int32_t step,
-                                                int32_t cache_cap) {
-  const int lane = threadIdx.x & 63;
-  SplitLens x = {0, 0};
-  if (lane < batch) {
-    const int32_t len = base_len[lane];
-    x.base = clamp_len(len, max_base);
-    if (!kPages || len >= 0) x.u = decode_units(min(x.base + step + 1, cache_cap));
-  }
-  return x;
-}
-__device__ __forceinline__ bool all_of(const SplitLens& x, int32_t units, int32_t batch) {
-  return __ballot((int)(threadIdx.x & 63) < batch && x.u != units) == 0;
-}
-template <bool kPages>
-__device__ __forceinline__ SplitDeal deal_splits(const SplitLens& x, int32_t batch, int32_t n_splits) {
-  const int lane = threadIdx.x & 63;
-  const int32_t u = x.u, u0 = __builtin_amdgcn_readfirstlane(u);
-  if (all_of(x, u0, batch)) {
-    if (kPages && u0 == 0) return {kDecodeUnit, 0, 0};   // nothing but padding
-    const int32_t s = min(n_splits, u0), cu = __builtin_amdgcn_readfirstlane(ceil_div24(u0, s, __builtin_amdgcn_rcpf((float)s)));
-    return {cu * kDecodeUnit, __builtin_amdgcn_readfirstlane(ceil_div24(u0, cu, __builtin_amdgcn_rcpf((float)cu))), 0};
-  }
-  int32_t total = 0, longest = 0;
-  for (int b = 0; b < batch; ++b) {
-    const int32_t ub = __builtin_amdgcn_readlane(u, b);
-    total += ub;
-    longest = max(longest, ub);
-  }
-  const RangeCandidates rc = decode_range_candidates(total, longest, n_splits, batch);
-  const int32_t c = rc.at(lane);   // lane i weighs candidate i
-  const float inv = __builtin_amdgcn_rcpf((float)c);
-  int32_t sum = 0;
-  for (int b = 0; b < batch; ++b) sum += ceil_div24(__builtin_amdgcn_readlane(u, b), c, inv);
-  const uint64_t fits = __ballot(sum <= n_splits * batch);   // (lane 63: always)
-  const int32_t cu = __builtin_amdgcn_readlane(c, __ffsll((unsigned long long)fits) - 1);
-  return {cu * kDecodeUnit, -1, ceil_div24(u, cu, __builtin_amdgcn_rcpf((float)cu))};
-}
-__device__ __forceinline__ SplitPlace place_of(const SplitDeal& d, int b) {   // b uniform
-  if (d.n >= 0) return {d.n, b * d.n};
-  SplitPlace p = {__builtin_amdgcn_readlane(d.mine, b), 0};
-  for (int i = 0; i < b; ++i) p.first += __builtin_amdgcn_readlane(d.mine, i);
-  return p;
-}
-
-// (x, y) turned by (c, s) in the float32 form of the re-rotation kernel.
-__device__ __forceinline__ void rot_pair(float& x, float& y, float c, float s) {
-  const float u = x, v = y;
-  x = fmaf(u, c, -(v * s));
-  y = fmaf(u, s, v * c);
-}
-__device__ __forceinline__ void unpack8(u32x4 w, float (&x)[8]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    x[2 * e] = __uint_as_float(w[e] << 16);
-    x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-  }
-}
-__device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
-  return u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-               pack_bf16x2(x[6], x[7])};
-}
-// The head dims 32 ks + 8 g4 .. + 8 (ks < HD/32) a lane holds of one row (the A / B operand
-// layout below), turned by row `trow` of the table: rotate-half pairs are chunks ks and
-// ks + HD/64 (frequencies 32 ks + 8 g4 + j), interleaved pairs sit inside a chunk (16 ks + 4 g4 + m).
-template <int HD, bool kInterleaved>
-__device__ __forceinline__ void rot_operand(u32x4 (&c)[Dims<HD>::kSteps], const float2* trow, int g4) {
-  constexpr int KS = Dims<HD>::kSteps;
-  if constexpr (!kInterleaved) {
-#pragma unroll
-    for (int ks = 0; ks < KS / 2; ++ks) {
-      float x[8], y[8];
-      unpack8(c[ks], x);
-      unpack8(c[ks + KS / 2], y);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float2 cs = trow[32 * ks + 8 * g4 + j];
-        rot_pair(x[j], y[j], cs.x, cs.y);
-      }
-      c[ks] = pack8(x);
-      c[ks + KS / 2] = pack8(y);
-    }
-  } else {
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      float x[8];
-      unpack8(c[ks], x);
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const float2 cs = trow[16 * ks + 4 * g4 + m];
-        rot_pair(x[2 * m], x[2 * m + 1], cs.x, cs.y);
-      }
-      c[ks] = pack8(x);
-    }
-  }
-}
 
 // grid (S * B * Hkv, L), 256 threads.  kDealt: ranges dealt by length (decode_dealt), else n_splits equal
 // ones (a kernel of its own: tested in the kernel, the choice cost launches of 1600 short contexts 1 %).
-// kPages: the cache is handed out in pages of 1 << shift >= 16 tokens.  A tile's two blocks of 16 keys
-// lie in one page each, so a wave needs two page numbers per tile; it holds the table's next 64
-// entries in a register (lane j: entry win + j) and takes them out with readlane, the 64 after those on
-// their way, so that no tile's loads wait for the table.
-template <int HD, bool kRope, bool kInterleaved, bool kDealt, bool kPages>
+template <int HD, bool kRope, bool kInterleaved, bool kDealt>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 decode_bf16_kernel(DecodeArgs a) {
   constexpr int kHD = HD, kRowBytes = Dims<HD>::kRowBytes, kVTileBytes = Dims<HD>::kVTileBytes;
@@ -254,7 +86,7 @@ decode_bf16_kernel(DecodeArgs a) {
     place = {a.n_splits, b * a.n_splits};
     base = clamp_len(a.base_len[b], a.max_base);
   } else {
-    const SplitLens lens = split_lens<kPages>(a.base_len, a.batch, a.max_base, a.step, a.cache_cap);
+    const SplitLens lens = split_lens<false>(a.base_len, a.batch, a.max_base, a.step, a.cache_cap);
     const int bg = at / a.eq.n;
     split = at % a.eq.n;
     b = bg / a.n_kv_heads;
@@ -262,8 +94,7 @@ decode_bf16_kernel(DecodeArgs a) {
     place = {a.eq.n, b * a.eq.n};
     chunk = a.eq.chunk;
     if (!all_of(lens, a.eq.units, a.batch)) {
-      const SplitDeal deal = deal_splits<kPages>(lens, a.batch, a.n_splits);
-      if (kPages && deal.n == 0) return;   // (uniform) a batch of padding
+      const SplitDeal deal = deal_splits<false>(lens, a.batch, a.n_splits);
       chunk = deal.chunk;
       if (deal.n >= 0) {
         b = at / (deal.n * a.n_kv_heads);
@@ -298,46 +129,18 @@ decode_bf16_kernel(DecodeArgs a) {
   const int c1 = min(c0 + sub, wc1);
 
   const int64_t bh_kv = (((int64_t)l * a.batch + b) * a.n_kv_heads + g);
-  const int64_t row0 = kPages ? ((int64_t)l * a.n_kv_heads + g) * a.stream_rows : 0;   // (pages) the stream's rows
-  const bf16_t* Kg = a.cache_k + (kPages ? row0 * kHD : bh_kv * a.cache_cap * kHD);
-  const bf16_t* Vg = a.cache_v + (kPages ? row0 * kHD : bh_kv * a.cache_cap * kHD);
+  const bf16_t* Kg = a.cache_k + bh_kv * a.cache_cap * kHD;
+  const bf16_t* Vg = a.cache_v + bh_kv * a.cache_cap * kHD;
   const bf16_t* Kn = a.k_new + bh_kv * kHD;
   const bf16_t* Vn = a.v_new + bh_kv * kHD;
-
-  // pages: entries [win, win + 64) and the 64 after them, for a range from slot `first` on (which does
-  // not wait for the lengths); the page of the new token, for its store at the end
-  const int32_t* ptab = kPages ? a.map.table + (int64_t)b * a.map.cap : nullptr;
-  int32_t win = 0, w_cur = 0, w_next = 0;
-  int64_t store_row = -1;
-  auto entry = [&](int32_t i) { return ptab[clamp_entry(i, a.map)]; };
-  if constexpr (kPages) {
-    const int64_t first = min((int64_t)split * chunk + wave * sub, (int64_t)a.cache_cap - 1);
-    win = (int32_t)(first >> a.map.shift);
-    w_cur = entry(win + lane);
-    w_next = entry(win + 64 + lane);
-    if constexpr (!kDealt) {
-      if (a.base_len[b] < 0) return;   // (uniform) padding of the batch
-    }
-  }
-  // the row that slot k0, a multiple of 16 (k0 >= the last one asked for), lies in
-  auto page_at = [&](int k0) -> int32_t {   // k0 uniform
-    const int32_t i = k0 >> a.map.shift;
-    if (i >= win + 64) {
-      win += 64;
-      w_cur = w_next;
-      w_next = entry(win + 64 + lane);
-    }
-    const int32_t page = clamp_page(__builtin_amdgcn_readlane(w_cur, i - win), a.map);
-    return (page << a.map.shift) + (k0 & ((1 << a.map.shift) - 1));
-  };
 
   // The workgroup holding slot p writes the new token into the cache.  Nobody reads that row
   // from the cache during this launch: the wave whose range holds it reads k_new / v_new.
   const float2* trow = kRope ? a.table + (int64_t)l * a.table_stride + (int64_t)min(p, a.max_abs_delta) * (kHD / 2)
                              : nullptr;   // rope variant: cos/sin of position p
-  auto store_new = [&](int64_t row) {
+  if (hgrp == 0 && p < a.cache_cap && p >= wc0 && p < wc1 && wave == 0 && lane < 2 * KC) {
     const int c = lane & (KC - 1);   // lanes [0, KC): K chunks, [KC, 2 KC): V chunks
-    u32x4* dst = reinterpret_cast<u32x4*>((lane < KC ? a.cache_k : a.cache_v) + row * kHD);
+    u32x4* dst = reinterpret_cast<u32x4*>((lane < KC ? a.cache_k : a.cache_v) + (bh_kv * a.cache_cap + p) * kHD);
     if (kRope && lane < KC) {   // the new key turned to p: lane c < KC/2 takes a chunk pair
       if (c < KC / 2) {
         // rotate-half: chunks c, c + KC/2 (frequencies 8 c ..); interleaved: 2 c, 2 c + 1 (8 c ..)
@@ -361,12 +164,6 @@ decode_bf16_kernel(DecodeArgs a) {
     } else {
       dst[c] = reinterpret_cast<const u32x4*>(lane < KC ? Kn : Vn)[c];
     }
-  };
-  const bool stores = hgrp == 0 && p < a.cache_cap && p >= wc0 && p < wc1 && wave == 0 && lane < 2 * KC;
-  if constexpr (kPages) {   // (stored after the key loop: nothing there waits for the entry)
-    if (stores) store_row = page_store_row(a.map, b, p);
-  } else if (stores) {
-    store_new(bh_kv * a.cache_cap + p);
   }
 
   const int n = lane & 15, g4 = lane >> 4;
@@ -386,22 +183,11 @@ decode_bf16_kernel(DecodeArgs a) {
 
   // K of one tile, straight into the A-operand layout: [mb][ks] = row k0 + 16 mb + n, head
   // dims 32 ks + 8 g4 .. +8.  Rows past the range are clamped (their scores are masked).
-  // (pages: blk16[mb] = (slot, row) of the tile's blocks of 16 keys; a block past the range is its last
-  // block again)
-  int blk_slot[2] = {0, 0};
-  int32_t blk_row[2] = {0, 0};
-  auto find_blocks = [&](int k0) {
-#pragma unroll
-    for (int mb = 0; mb < 2; ++mb) {
-      blk_slot[mb] = min(k0 + 16 * mb, (c1 - 1) & ~15);
-      blk_row[mb] = page_at(blk_slot[mb]);
-    }
-  };
   auto load_k = [&](int k0, u32x4 (&kr)[2][KS]) {
 #pragma unroll
     for (int mb = 0; mb < 2; ++mb) {
-      const int row = min((kPages ? blk_slot[mb] : k0 + 16 * mb) + n, c1 - 1);
-      const bf16_t* src = row == p ? Kn : Kg + (kPages ? (int64_t)blk_row[mb] + (row - blk_slot[mb]) : (int64_t)row) * kHD;
+      const int row = min(k0 + 16 * mb + n, c1 - 1);
+      const bf16_t* src = row == p ? Kn : Kg + (int64_t)row * kHD;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
         kr[mb][ks] = *reinterpret_cast<const u32x4*>(src + 32 * ks + 8 * g4);
@@ -414,11 +200,10 @@ decode_bf16_kernel(DecodeArgs a) {
   auto load_v = [&](int k0, uint8_t* buf) {
 #pragma unroll
     for (int i = 0; i < kTile / RPM; ++i) {
-      const int rl = RPM * i + ld_r, mb = RPM * i / 16;
-      const int row = min(kPages ? blk_slot[mb] + (RPM * i & 15) + ld_r : k0 + rl, c1 - 1);
+      const int rl = RPM * i + ld_r;
+      const int row = min(k0 + rl, c1 - 1);
       const int c = ld_slot ^ v_swz<HD>(rl);
-      const bf16_t* src =
-          (row == p ? Vn : Vg + (kPages ? (int64_t)blk_row[mb] + (row - blk_slot[mb]) : (int64_t)row) * kHD) + 8 * c;
+      const bf16_t* src = (row == p ? Vn : Vg + (int64_t)row * kHD) + 8 * c;
       __builtin_amdgcn_global_load_lds((const GLOBAL_AS void*)src,
                                        (LDS_AS void*)(buf + wave * kVTileBytes + RPM * i * kRowBytes), 16, 0,
                                        kNonTemporal);
@@ -453,7 +238,6 @@ decode_bf16_kernel(DecodeArgs a) {
     const uint8_t* vcur = P ? v_lds1 : v_lds0;
     uint8_t* vnext = P ? v_lds0 : v_lds1;
     if (k0 + kTile < c1) {
-      if constexpr (kPages) find_blocks(k0 + kTile);
       load_k(k0 + kTile, knext);
       load_v(k0 + kTile, vnext);
     }
@@ -515,7 +299,6 @@ decode_bf16_kernel(DecodeArgs a) {
 
   u32x4 k_a[2][KS], k_b[2][KS];
   if (c0 < c1) {
-    if constexpr (kPages) find_blocks(c0);
     load_k(c0, k_a);
     load_v(c0, v_lds0);
     __builtin_amdgcn_s_waitcnt(0x0F70);
@@ -523,10 +306,6 @@ decode_bf16_kernel(DecodeArgs a) {
       tile(k0, std::integral_constant<int, 0>{}, k_a, k_b);
       if (k0 + kTile < c1) tile(k0 + kTile, std::integral_constant<int, 1>{}, k_b, k_a);
     }
-  }
-
-  if constexpr (kPages) {
-    if (store_row >= 0) store_new(row0 + store_row);
   }
 
   // ---- merge the 4 waves (log-sum-exp) through LDS, reusing the V buffers
@@ -584,117 +363,27 @@ decode_bf16_kernel(DecodeArgs a) {
   }
 }
 
-// grid (rows, L), 256 threads, rows [row0, row0 + grid) of the B * Hq: merge the ranges of one query
-// head by log-sum-exp.  HD / 4 lanes
-// hold 4 head dims each of one range, 1024 / HD ranges side by side, and every range's loads are
-// issued before any is used; the range groups then merge in LDS.  (One wave walking the ranges
-// took 4.9 us for 8 or 32 of them: a memory round trip per 8, once for the maxima and once for
-// the sums.)  A range that saw no key (maximum -inf) adds nothing.
-template <int HD, bool kDealt, bool kPages>
-__global__ void __launch_bounds__(256) decode_combine_kernel(const float* __restrict__ ws_o,
-                                                             const float* __restrict__ ws_ml,
-                                                             const int32_t* __restrict__ base_len, int32_t batch,
-                                                             int32_t n_q_heads, int32_t max_base, int32_t step,
-                                                             int32_t cache_cap, int32_t n_splits, EqualDeal eq,
-                                                             int32_t row0, bf16_t* __restrict__ out) {
-  constexpr int kLanes = HD / 4, kGroups = 256 / kLanes, kBatch = 4;
-  __shared__ float m_s[kGroups], l_s[kGroups];
-  __shared__ __attribute__((aligned(16))) float o_s[kGroups * HD];
-  const int bh = row0 + blockIdx.x, b = bh / n_q_heads, h = bh - b * n_q_heads, l = blockIdx.y;
-  const int grp = threadIdx.x / kLanes, d = 4 * (threadIdx.x % kLanes);
-  const int64_t layer0 = (int64_t)l * batch * n_splits * n_q_heads;   // (slots)
-  const int32_t n0 = kDealt ? eq.n : n_splits;
-  SplitPlace place = {n0, b * n0};
-  float2 ml[kBatch];
-  f32x4_t x[kBatch];
-  auto load = [&](int s0) {
-    const int64_t slot0 = layer0 + (int64_t)place.first * n_q_heads + (int64_t)h * place.n;
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      const int s = s0 + u * kGroups;
-      ml[u] = s < place.n ? *reinterpret_cast<const float2*>(ws_ml + 2 * (slot0 + s)) : make_float2(-INFINITY, 0.f);
-      x[u] = s < place.n ? *reinterpret_cast<const f32x4_t*>(ws_o + (slot0 + s) * HD + d) : f32x4_t{};
-    }
-  };
-  if constexpr (kDealt) {
-    const SplitLens lens = split_lens<kPages>(base_len, batch, max_base, step, cache_cap);
-    load(grp);   // (equal ranges fit the array whatever the lengths are)
-    if (!all_of(lens, eq.units, batch)) {
-      place = place_of(deal_splits<kPages>(lens, batch, n_splits), b);
-      load(grp);
-    }
-    // (uniform) a whole request: its output is stored; padding: there is none
-    if (kPages ? place.n <= 1 : place.n == 1) return;
-  } else {
-    load(grp);
-    if (kPages && base_len[b] < 0) return;   // (uniform) padding of the batch
-  }
-  float M = -INFINITY, den = 0.f;
-  f32x4_t o = {};
-  for (int s0 = grp; s0 < place.n; s0 += kBatch * kGroups) {
-    if (s0 != grp) load(s0);
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      if (ml[u].x == -INFINITY) continue;
-      const float m_new = fmaxf(M, ml[u].x);
-      const float keep = __builtin_amdgcn_exp2f(M - m_new), w = __builtin_amdgcn_exp2f(ml[u].x - m_new);
-      M = m_new;
-      den = den * keep + w * ml[u].y;
-      o = o * keep + w * x[u];
-    }
-  }
-  *reinterpret_cast<f32x4_t*>(o_s + grp * HD + d) = o;
-  if (d == 0) {
-    m_s[grp] = M;
-    l_s[grp] = den;
-  }
-  __syncthreads();
-  if (threadIdx.x >= HD / 2) return;
-  float m_all = -INFINITY;
-#pragma unroll
-  for (int g = 0; g < kGroups; ++g) m_all = fmaxf(m_all, m_s[g]);
-  float l_all = 0.f, o0 = 0.f, o1 = 0.f;
-#pragma unroll
-  for (int g = 0; g < kGroups; ++g) {
-    if (m_s[g] == -INFINITY) continue;
-    const float w = __builtin_amdgcn_exp2f(m_s[g] - m_all);
-    l_all += w * l_s[g];
-    o0 += w * o_s[g * HD + 2 * threadIdx.x];
-    o1 += w * o_s[g * HD + 2 * threadIdx.x + 1];
-  }
-  const float inv = 1.f / l_all;
-  const int64_t row = ((int64_t)l * batch + b) * n_q_heads + h;
-  reinterpret_cast<uint32_t*>(out + row * HD)[threadIdx.x] = pack_bf16x2(o0 * inv, o1 * inv);
-}
-
-template <int HD, bool kDealt, bool kPages>
+template <int HD, bool kDealt>
 hipError_t launch_decode_as(const DecodeArgs& a, dim3 grid, bool rope, bool interleaved, const AttnShape& s,
                             hipStream_t stream) {
   if (!rope)
-    hipLaunchKernelGGL((decode_bf16_kernel<HD, false, false, kDealt, kPages>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((decode_bf16_kernel<HD, false, false, kDealt>), grid, dim3(256), 0, stream, a);
   else if (interleaved)
-    hipLaunchKernelGGL((decode_bf16_kernel<HD, true, true, kDealt, kPages>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((decode_bf16_kernel<HD, true, true, kDealt>), grid, dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL((decode_bf16_kernel<HD, true, false, kDealt, kPages>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((decode_bf16_kernel<HD, true, false, kDealt>), grid, dim3(256), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_splits == 1) return e;
-  // (a grid holds fewer than 2^32 threads per dimension)
-  const int64_t rows = (int64_t)s.batch * s.n_q_heads, kPart = int64_t(1) << 23;
-  for (int64_t row0 = 0; row0 < rows && e == hipSuccess; row0 += kPart) {
-    hipLaunchKernelGGL((decode_combine_kernel<HD, kDealt, kPages>), dim3((unsigned)std::min(rows - row0, kPart), s.n_layers),
-                       dim3(256), 0, stream, a.ws_o, a.ws_ml, a.base_len, s.batch, s.n_q_heads, a.max_base, a.step,
-                       a.cache_cap, a.n_splits, a.eq, (int32_t)row0, a.out);
-    e = hipGetLastError();
-  }
-  return e;
+  return launch_decode_combine<HD, kDealt, false>(a.ws_o, a.ws_ml, a.base_len, s, a.max_base, a.step, a.cache_cap, a.n_splits,
+                                                  a.eq, a.out, stream);
 }
 
-template <int HD, bool kPages>
+template <int HD>
 hipError_t launch_decode_hd(const DecodeArgs& a, dim3 grid, bool rope, bool interleaved, const AttnShape& s,
                             hipStream_t stream) {
   return decode_dealt(a.n_splits, a.batch, a.max_base + a.step + 1)
-             ? launch_decode_as<HD, true, kPages>(a, grid, rope, interleaved, s, stream)
-             : launch_decode_as<HD, false, kPages>(a, grid, rope, interleaved, s, stream);
+             ? launch_decode_as<HD, true>(a, grid, rope, interleaved, s, stream)
+             : launch_decode_as<HD, false>(a, grid, rope, interleaved, s, stream);
 }
 
 }  // namespace
@@ -722,80 +411,49 @@ hipError_t decode_scratch_ptr(void** out) {
   return hipSuccess;
 }
 
-namespace {
-
-// `a` as far as a call's buffers and lengths go; fills in what follows from the shape, and launches.
-template <bool kPages>
-hipError_t launch_decode(DecodeArgs a, const AttnShape& s, int32_t n_splits, void* workspace, bool interleaved,
-                         hipStream_t stream) {
-  if (s.batch == 0 || s.n_layers == 0) return hipSuccess;
-  const int32_t max_len = a.max_base + a.step + 1;
-  const size_t rows = (size_t)s.n_layers * s.batch * s.n_q_heads * n_splits;
-  a.ws_o = static_cast<float*>(workspace);
-  a.ws_ml = a.ws_o ? a.ws_o + rows * s.head_dim : nullptr;
-  a.batch = s.batch;
-  a.n_q_heads = s.n_q_heads;
-  a.n_kv_heads = s.n_kv_heads;
-  a.n_splits = n_splits;
-  const int32_t chunk = ceil_div(max_len, n_splits);
-  a.chunk = (int32_t)min((int64_t)decode_units(chunk) * kDecodeUnit, (int64_t)INT32_MAX / kDecodeUnit * kDecodeUnit);
-  a.eq = {};
-  if (decode_dealt(n_splits, s.batch, max_len)) {
-    a.eq.units = decode_units(std::min(max_len, a.cache_cap));
-    const int32_t per = ceil_div(a.eq.units, std::min(n_splits, a.eq.units));   // units per range
-    a.eq.n = ceil_div(a.eq.units, per);
-    a.eq.chunk = per * kDecodeUnit;
-  }
-  a.scale_log2 = s.scale_log2;
-  a.head_groups = decode_head_groups(s);
-  const dim3 grid(a.head_groups * n_splits * s.batch * s.n_kv_heads, s.n_layers);
-  if (s.head_dim == 64) return launch_decode_hd<64, kPages>(a, grid, a.table != nullptr, interleaved, s, stream);
-  return launch_decode_hd<128, kPages>(a, grid, a.table != nullptr, interleaved, s, stream);
-}
-
-}  // namespace
-
 hipError_t launch_decode_bf16(const AttnShape& s, const bf16_t* q, const bf16_t* k_new,
                               const bf16_t* v_new, bf16_t* cache_k, bf16_t* cache_v,
                               const int32_t* base_len, int32_t max_base, int32_t step,
                               int32_t n_splits, bf16_t* out, void* workspace, size_t,
                               const float2* rope_table, int64_t table_stride, int32_t max_abs_delta,
                               bool interleaved, hipStream_t stream) {
-  DecodeArgs a = {};
+  if (s.batch == 0 || s.n_layers == 0) return hipSuccess;
+  const int32_t max_len = max_base + step + 1;
+  DecodeArgs a;
   a.q = q;
   a.k_new = k_new;
   a.v_new = v_new;
   a.cache_k = cache_k;
   a.cache_v = cache_v;
-  a.cache_cap = s.cache_cap;
   a.base_len = base_len;
   a.out = out;
+  const size_t rows = (size_t)s.n_layers * s.batch * s.n_q_heads * n_splits;
+  a.ws_o = static_cast<float*>(workspace);
+  a.ws_ml = a.ws_o ? a.ws_o + rows * s.head_dim : nullptr;
+  a.batch = s.batch;
+  a.cache_cap = s.cache_cap;
+  a.n_q_heads = s.n_q_heads;
+  a.n_kv_heads = s.n_kv_heads;
   a.max_base = max_base;
   a.step = step;
+  a.n_splits = n_splits;
+  const int32_t chunk = ceil_div(max_len, n_splits);
+  a.chunk = (int32_t)min((int64_t)decode_units(chunk) * kDecodeUnit, (int64_t)INT32_MAX / kDecodeUnit * kDecodeUnit);
+  a.eq = {};
+  if (decode_dealt(n_splits, s.batch, max_len)) {
+    a.eq.units = decode_units(std::min(max_len, s.cache_cap));
+    const int32_t per = ceil_div(a.eq.units, std::min(n_splits, a.eq.units));   // units per range
+    a.eq.n = ceil_div(a.eq.units, per);
+    a.eq.chunk = per * kDecodeUnit;
+  }
+  a.scale_log2 = s.scale_log2;
   a.table = rope_table;
   a.table_stride = table_stride;
   a.max_abs_delta = max_abs_delta;
-  return launch_decode<false>(a, s, n_splits, workspace, interleaved, stream);
-}
-
-hipError_t launch_decode_bf16_pages(const PageAttnArgs& p) {
-  DecodeArgs a = {};
-  a.q = static_cast<const bf16_t*>(p.q);
-  a.k_new = static_cast<const bf16_t*>(p.k_new);
-  a.v_new = static_cast<const bf16_t*>(p.v_new);
-  a.cache_k = static_cast<bf16_t*>(p.pages_k);
-  a.cache_v = static_cast<bf16_t*>(p.pages_v);
-  a.cache_cap = (int32_t)std::min((int64_t)p.map.cap << p.map.shift, (int64_t)INT32_MAX);
-  a.base_len = p.base_len;
-  a.out = static_cast<bf16_t*>(p.out);
-  a.max_base = p.max_base;
-  a.step = p.offset;
-  a.table = p.table;
-  a.table_stride = p.table_stride;
-  a.max_abs_delta = p.max_abs_delta;
-  a.map = p.map;
-  a.stream_rows = p.s.cache_cap;
-  return launch_decode<true>(a, p.s, p.n_splits, p.workspace, p.interleaved, p.stream);
+  a.head_groups = decode_head_groups(s);
+  const dim3 grid(a.head_groups * n_splits * s.batch * s.n_kv_heads, s.n_layers);
+  if (s.head_dim == 64) return launch_decode_hd<64>(a, grid, rope_table != nullptr, interleaved, s, stream);
+  return launch_decode_hd<128>(a, grid, rope_table != nullptr, interleaved, s, stream);
 }
 
 }  // namespace pic

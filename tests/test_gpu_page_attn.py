@@ -20,7 +20,7 @@ HEADS = [(4, 2, 64), (32, 8, 128), (28, 4, 128), (5, 1, 64), (3, 3, 128), (40, 1
 def test_decode(dtype, hq, hkv, d, P):
     x = setup(hq, hkv, d, dtype, P, [0, 1, 15, 16, 17, 63, 64, 65, 300, -1, 511], [1] * 11)
     decode(x)
-    check(x)
+    check(x, decoded=True)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -29,7 +29,7 @@ def test_decode_few_rows(dtype, ctx):
     for P in (16, 128, 1024):
         x = setup(8, 2, 128, dtype, P, ctx, [1] * len(ctx), slack=5)
         decode(x, step=0)
-        check(x)
+        check(x, decoded=True)
 
 
 @pytest.mark.parametrize("n_splits", [1, 2, 3, 8, 13, 64])
@@ -38,7 +38,7 @@ def test_decode_splits(n_splits, P):
     # uneven contexts, some shorter than the ranges a split gives them, padding in between
     x = setup(16, 4, 128, "bf16", P, [3000, -1, 5, 1029, 8400, 0, -1, 4096], [1] * 8, slack=77)
     decode(x, n_splits=n_splits)
-    check(x)
+    check(x, decoded=True)
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -47,32 +47,7 @@ def test_decode_dealt_ranges_with_padding(d, base):
     # 8 splits and long contexts: ranges dealt by length, padding gets none
     x = setup(8, 2, d, "bf16", 64, base, [1, 1, 1], slack=12000 - max(max(base), 0))
     decode(x, n_splits=8)
-    check(x)
-
-
-@pytest.mark.parametrize("hq,hkv,d,n_splits,base", [
-    (32, 8, 128, 0, [700, 64, 3]), (28, 4, 128, 0, [5000]), (8, 8, 64, 3, [1000, 2049]), (40, 2, 128, 5, [300, 900]),
-    (8, 2, 128, 8, [9000, 500, 12000]), (8, 2, 64, 8, [9000, 9000]), (32, 8, 128, 1, [40] * 40)])
-@pytest.mark.parametrize("rope", [False, True])
-def test_decode_bits_of_the_contiguous_call(hq, hkv, d, n_splits, base, rope):
-    for P in (16, 64):
-        x = setup(hq, hkv, d, "bf16", P, base, [1] * len(base), L=2)
-        ck, cv, cap = contiguous(x)
-        r = rope_table(x) if rope else None
-        decode(x, n_splits=n_splits, rope=r)
-        ws = torch.empty(max(pic.pic_decode_workspace_bytes(x.model, x.B, x.max_ctx + 1, n_splits), 16), dtype=torch.uint8,
-                         device=DEV)
-        out = torch.empty_like(x.out)
-        args = (x.model, x.q, x.k, x.v, ck, cv, x.B, cap, x.len, 0, x.max_ctx)
-        if rope:
-            pic.pic_decode_attn_rope(*args, *r, out, ws, n_splits)
-        else:
-            pic.pic_decode_attn(*args, out, ws, n_splits)
-        assert (out == x.out).all()
-        for b in range(x.B):
-            r0 = rows(x, b, 0, base[b] + 1)
-            for p, c in ((x.pk, ck), (x.pv, cv)):
-                assert (p[:, :, r0] == c[:, b, :, : base[b] + 1]).all()
+    check(x, decoded=True)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -80,7 +55,7 @@ def test_decode_bits_of_the_contiguous_call(hq, hkv, d, n_splits, base, rope):
 def test_decode_step_and_layers(dtype, step):
     x = setup(8, 4, 64, dtype, 32, [step, 100 + step, 77 + step], [1] * 3, L=3, slack=9)
     decode(x, step=step, scale=0.07)
-    check(x, scale=0.07)
+    check(x, scale=0.07, decoded=True)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -179,7 +154,7 @@ def test_rope_is_turning_first(kind, pairing, d):
     for b in range(y.B):   # and those outputs are right
         m = y.new[b] if ctx[b] >= 0 else 0
         y.K[b] = torch.cat([y.K[b][:, :, : y.K[b].shape[2] - m], y.k[:, b, :m].transpose(1, 2)], 2)
-    check(y)
+    check(y, decoded=kind == "decode")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -191,7 +166,7 @@ def test_large_scores(dtype):
         x.K[b][:, :, t] *= 6
     x.q *= 4
     decode(x)
-    check(x)
+    check(x, decoded=True)
 
 
 @pytest.mark.parametrize("kind", ["decode", "suffix"])
@@ -229,7 +204,7 @@ def test_lengths_are_clamped():
     x = setup(8, 2, 128, "bf16", 16, [40, 33], [1, 1])
     x.len = torch.tensor([2**31 - 1, 33], dtype=torch.int32, device=DEV)
     decode(x)
-    check(x)
+    check(x, decoded=True)
     x = setup(8, 2, 128, "bf16", 16, [40, 33], [3, 3])
     x.len = torch.tensor([1 << 20, 33], dtype=torch.int32, device=DEV)
     x.n_valid = torch.tensor([2**31 - 1, 3], dtype=torch.int32, device=DEV)
@@ -264,7 +239,7 @@ def test_rows_past_32_bits():
             ok[rows(x, b, 0, x.K[b].shape[2])] = True
         x.pk[:, :, ~ok] = float("nan")
         x.pv[:, :, ~ok] = float("nan")
-        check(x)
+        check(x, decoded=True)
 
 
 def test_binding_refusals():
@@ -282,4 +257,4 @@ def test_binding_refusals():
         decode(x, n_splits=4, ws=None)
     assert (x.out == SENTINEL).all()
     decode(x)
-    check(x)
+    check(x, decoded=True)
