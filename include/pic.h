@@ -490,9 +490,10 @@ pic_status pic_page_copy(const pic_model* model, const pic_pages* pages, void* p
 
 /* ---- 5c. suffix prefill over pages ----
    pic_suffix_prefill_attn on a paged cache: stores k_suf / v_suf of token i < n_valid[b] of request
-   b at slot ctx_len[b] + i and computes its attention over slots [0, ctx_len[b] + i].  Outputs are
-   bit-identical to pic_suffix_prefill_attn's on the same cache contents with the same workspace, where
-   every token is valid.
+   b at slot ctx_len[b] + i and computes its attention over slots [0, ctx_len[b] + i].  Up to 32 query rows
+   (tokens x query heads) per kv head may run on a kernel of their own, which keeps probabilities to 16
+   bits; otherwise outputs are pic_suffix_prefill_attn's bit for bit, on the same cache contents with
+   the same workspace.
      page_table [device, batch x table_cap]
      ctx_len    [device, batch]   clamped to max_ctx; a negative one marks a request that is only
                                   padding: nothing of it is read, stored or computed

@@ -18,7 +18,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["pic_api.cpp", "pic_pages.cpp", "pic_plan.cpp", "rope_compose.hip", "attn_f32.hip", "prefill_bf16.hip",
-           "decode_bf16.hip", "page_decode.hip", "page_copy.hip"]
+           "decode_bf16.hip", "page_decode.hip", "page_few.hip", "page_copy.hip"]
 
 CFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17", "-fvisibility=hidden",

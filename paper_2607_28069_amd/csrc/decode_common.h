@@ -177,13 +177,18 @@ __device__ __forceinline__ void rot_operand(u32x4 (&c)[Dims<HD>::kSteps], const 
 // issued before any is used; the range groups then merge in LDS.  (One wave walking the ranges
 // took 4.9 us for 8 or 32 of them: a memory round trip per 8, once for the maxima and once for
 // the sums.)  A range that saw no key (maximum -inf) adds nothing.
+// (pages, heads > 0: `heads` query rows for each of n_new tokens per request, n_q_heads counting them all)
+struct FewTokens {
+  const int32_t* n_valid = nullptr;
+  int32_t n_new = 1, heads = 0;
+};
 template <int HD, bool kDealt, bool kPages>
 __global__ void __launch_bounds__(256) decode_combine_kernel(const float* __restrict__ ws_o,
                                                              const float* __restrict__ ws_ml,
                                                              const int32_t* __restrict__ base_len, int32_t batch,
                                                              int32_t n_q_heads, int32_t max_base, int32_t step,
                                                              int32_t cache_cap, int32_t n_splits, EqualDeal eq,
-                                                             int32_t row0, bf16_t* __restrict__ out) {
+                                                             int32_t row0, bf16_t* __restrict__ out, FewTokens few) {
   constexpr int kLanes = HD / 4, kGroups = 256 / kLanes, kBatch = 4;
   __shared__ float m_s[kGroups], l_s[kGroups];
   __shared__ __attribute__((aligned(16))) float o_s[kGroups * HD];
@@ -214,7 +219,9 @@ __global__ void __launch_bounds__(256) decode_combine_kernel(const float* __rest
     if (kPages ? place.n <= 1 : place.n == 1) return;
   } else {
     load(grp);
-    if (kPages && base_len[b] < 0) return;   // (uniform) padding of the batch
+    // (uniform) padding of the batch, or of the request's tokens
+    if (kPages && (few.heads > 0 ? h / few.heads >= page_new_tokens(base_len, few.n_valid, b, few.n_new) : base_len[b] < 0))
+      return;
   }
   float M = -INFINITY, den = 0.f;
   f32x4_t o = {};
@@ -259,14 +266,14 @@ __global__ void __launch_bounds__(256) decode_combine_kernel(const float* __rest
 template <int HD, bool kDealt, bool kPages>
 hipError_t launch_decode_combine(const float* ws_o, const float* ws_ml, const int32_t* base_len, const AttnShape& s,
                                  int32_t max_base, int32_t step, int32_t cache_cap, int32_t n_splits, const EqualDeal& eq,
-                                 bf16_t* out, hipStream_t stream) {
+                                 bf16_t* out, hipStream_t stream, const FewTokens& few = FewTokens()) {
   // (a grid holds fewer than 2^32 threads per dimension)
   hipError_t e = hipSuccess;
   const int64_t rows = (int64_t)s.batch * s.n_q_heads, kPart = int64_t(1) << 23;
   for (int64_t row0 = 0; row0 < rows && e == hipSuccess; row0 += kPart) {
     hipLaunchKernelGGL((decode_combine_kernel<HD, kDealt, kPages>), dim3((unsigned)std::min(rows - row0, kPart), s.n_layers),
                        dim3(256), 0, stream, ws_o, ws_ml, base_len, s.batch, s.n_q_heads, max_base, step, cache_cap, n_splits,
-                       eq, (int32_t)row0, out);
+                       eq, (int32_t)row0, out, few);
     e = hipGetLastError();
   }
   return e;

@@ -330,13 +330,14 @@ page_decode_kernel(PageDecodeArgs a) {
   float l_tot = l_part + __shfl_xor(l_part, 16, 64);
   l_tot += __shfl_xor(l_tot, 32, 64);
   __syncthreads();
-  float* o_lds = reinterpret_cast<float*>(v_lds0);    // [4][16][HD] fp32: all of v_lds0
+  // [4][16][HD] fp32, all of v_lds0; 16-byte chunk c of row r at c ^ r: a store's rows would meet in one
+  // bank otherwise
+  auto o_lds = [&](int w, int r, int c) { return reinterpret_cast<f32x4_t*>(v_lds0) + (w * 16 + r) * (HD / 4) + (c ^ r); };
   float* ml_lds = reinterpret_cast<float*>(v_lds1);   // [4][16][2]
   if (n < n_here) {
 #pragma unroll
     for (int db = 0; db < DB; ++db)
-      *reinterpret_cast<float4*>(o_lds + (wave * 16 + n) * HD + 16 * db + 4 * g4) =
-          make_float4(oacc[db][0], oacc[db][1], oacc[db][2], oacc[db][3]);
+      *o_lds(wave, n, 4 * db + g4) = oacc[db];
     if (g4 == 0) {
       ml_lds[(wave * 16 + n) * 2] = m_run;
       ml_lds[(wave * 16 + n) * 2 + 1] = l_tot;
@@ -356,10 +357,12 @@ page_decode_kernel(PageDecodeArgs a) {
       if (mw == -INFINITY) continue;   // an empty wave range
       const float wt = __builtin_amdgcn_exp2f(mw - M);
       den += wt * ml_lds[(w * 16 + mn) * 2 + 1];
-      const float4 x0 = *reinterpret_cast<const float4*>(o_lds + (w * 16 + mn) * HD + md);
-      const float4 x1 = *reinterpret_cast<const float4*>(o_lds + (w * 16 + mn) * HD + md + 4);
-      o[0] += wt * x0.x; o[1] += wt * x0.y; o[2] += wt * x0.z; o[3] += wt * x0.w;
-      o[4] += wt * x1.x; o[5] += wt * x1.y; o[6] += wt * x1.z; o[7] += wt * x1.w;
+      const f32x4_t x0 = *o_lds(w, mn, md / 4), x1 = *o_lds(w, mn, md / 4 + 1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        o[e] += wt * x0[e];
+        o[4 + e] += wt * x1[e];
+      }
     }
     const int64_t row = ((int64_t)l * a.batch + b) * a.n_q_heads + g * n_rep + rep0 + mn;
     if (place.n == 1) {

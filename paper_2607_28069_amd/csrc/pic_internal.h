@@ -153,6 +153,12 @@ hipError_t launch_attn_f32_pages(const PageAttnArgs& a);
 hipError_t launch_decode_bf16_pages(const PageAttnArgs& a);
 // The prefill of bf16 pages: offset 0.
 hipError_t launch_prefill_bf16_pages(const PageAttnArgs& a);
+// The same for at most kFewRows query rows per kv head.
+constexpr int kFewRows = 32;
+hipError_t launch_few_bf16_pages(const PageAttnArgs& a);
+// Key ranges of such a launch, and whether it is the better one.
+bool few_bf16_better(const AttnShape& s, int32_t n_new, int32_t max_ctx, size_t ws_bytes);
+int32_t few_bf16_splits(const AttnShape& s, int32_t n_new, int32_t max_ctx, size_t ws_bytes);
 
 // Page pairs[i][1] = page pairs[i][0] in each of the n_streams (layer, kv head) streams of both
 // buffers; pages of page_bytes bytes, n_pages per stream.  `pairs` is host memory, read before the call returns.

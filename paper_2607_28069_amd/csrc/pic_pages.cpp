@@ -395,8 +395,10 @@ pic_status page_attn(const pic_model* model, const pic_pages* pages, const void*
   a.ws_bytes = ws_bytes;
   a.n_splits = n_splits;
   a.stream = (hipStream_t)stream;
+  const bool few = few_bf16_better(a.s, n_new, max_base, workspace ? ws_bytes : 0);
   const hipError_t e = model->dtype == PIC_F32 ? launch_attn_f32_pages(a)
                        : decode                ? launch_decode_bf16_pages(a)
+                       : few                   ? launch_few_bf16_pages(a)
                                                : launch_prefill_bf16_pages(a);
   return hip_status(e, decode ? "page decode launch" : "page suffix launch");
 }

@@ -179,6 +179,38 @@ size_t decode_bf16_auto_workspace(const AttnShape& s, int32_t max_len) {
   return decode_bf16_workspace(s, max_len, splits);
 }
 
+// Key ranges of a launch of few query rows over pages: one workgroup of eight waves per compute unit, each
+// wave keeping a tile of keys, as far as the workspace (sized for the prefill) holds their float32 partials.
+int32_t few_bf16_splits(const AttnShape& s, int32_t n_new, int32_t max_ctx, size_t ws_bytes) {
+  const int64_t pairs = (int64_t)s.batch * s.n_kv_heads * s.n_layers;
+  const size_t split_bytes = (size_t)s.n_layers * s.batch * n_new * s.n_q_heads * (s.head_dim + 2) * sizeof(float);
+  int64_t n = pairs > 0 ? 256 / pairs : 1;
+  n = std::min(n, ((int64_t)max_ctx + n_new + 255) / 256);
+  n = std::min(n, (int64_t)(ws_bytes / split_bytes));
+  return (int32_t)std::max<int64_t>(n, 1);
+}
+
+// Whether at most kFewRows query rows per kv head over pages go to the kernel that splits the keys over a
+// workgroup's waves, or to the prefill kernel.  Prefill / few, us, head_dim 128 (32 heads over 8), contexts of
+// 10K unless said: 16 requests x 4 tokens 131 / 117, x 8 133 / 123; 32 x 8 246 / 223; 40 x 8 417 / 344; 20 of 2K x 8
+// 46 / 33; one of 1K x 4 15.9 / 15.4, of 300 10.0 / 8.7; head_dim 64: 5 of 8K x 8 30.7 / 27.5, 16 of 4K x 8 41.7 / 30.7,
+// one of 1K x 4 13.2 / 9.2.  The prefill keeps
+//  * long contexts where the workspace, which holds twice as many of its bf16 partials, leaves so few ranges
+//    that half the compute units idle, each of which streams about 36 GB/s whatever runs on it (8 x 4, 128
+//    workgroups: 72 / 86; 8 of 33K, 28 heads over 4, x 2, 128: 104 / 129; 4 x 8, 128: 42.3 / 45.3; against 12 x 8,
+//    192: 115 / 98); at head_dim 64, where its waves are slower at half the bytes, below 80 (2 of 4K x 8, 64:
+//    14.8 / 15.5; one of 10K x 8, 80: 17.9 / 15.9);
+//  * two blocks of rows at head_dim 128, whose waves' results merge through 128 KB of LDS (2.5 us), over short
+//    contexts (16 of 300 x 8: 11.4 / 12.5; 32: 14.0 / 14.5).
+bool few_bf16_better(const AttnShape& s, int32_t n_new, int32_t max_ctx, size_t ws_bytes) {
+  const int64_t rows = (int64_t)n_new * (s.n_q_heads / s.n_kv_heads);
+  if (rows > kFewRows) return false;
+  const int64_t max_len = (int64_t)max_ctx + n_new, pairs = (int64_t)s.batch * s.n_kv_heads * s.n_layers;
+  const int32_t splits = few_bf16_splits(s, n_new, max_ctx, ws_bytes);
+  if (max_len >= 2048 && pairs * splits < (s.head_dim == 64 ? 80 : 160)) return false;
+  return s.head_dim == 64 || rows <= 16 || max_len >= 1024;
+}
+
 size_t decode_bf16_workspace(const AttnShape& s, int32_t, int32_t n_splits) {
   if (n_splits <= 1) return 0;
   const size_t rows = (size_t)s.n_layers * s.batch * s.n_q_heads * n_splits;

@@ -76,9 +76,39 @@ def test_suffix_lengths(dtype, n, ctx, P):
     check(x)
 
 
+@pytest.mark.parametrize("hq,hkv,d,n", [(32, 8, 128, 1), (32, 8, 128, 3), (32, 8, 128, 8), (28, 4, 128, 4), (4, 4, 128, 32),
+                                        (16, 1, 64, 2), (8, 8, 64, 13), (32, 8, 64, 8), (5, 1, 64, 3)])
+@pytest.mark.parametrize("batch", ["lone", "short", "uneven", "many"])
+def test_suffix_few_rows(hq, hkv, d, n, batch):
+    """Few enough rows for the kernel that splits the keys over waves: contexts that end anywhere in a wave's
+    tiles, ranges that hold new tokens only, tokens that a wave's keys all lie past."""
+    ctx = {"lone": [1900], "short": [0, 1, 33, 255, 256, 700], "uneven": [3000, -1, 2047, 0, 2560, 31],
+           "many": [2100 - 61 * i for i in range(30)]}[batch]
+    new = [max(n - i % (n + 1), 0) if batch != "lone" else n for i in range(len(ctx))]
+    for P, rope in ((16, False), (64, True)):
+        x = setup(hq, hkv, d, "bf16", P, ctx, new, n=n, slack=3)
+        if rope:   # against the turned rows
+            y = setup(hq, hkv, d, "bf16", P, ctx, new, n=n, slack=3)
+            r = rope_table(x)
+            pos = torch.tensor([[max(c, 0) + i for i in range(n)] for c in ctx], dtype=torch.int32, device=DEV)
+            for t, h in ((y.q, hq), (y.k, hkv)):
+                pic.pic_rerotate_keys(y.model, t, t, y.B * n, h, pos, *r)
+            suffix(x, rope=r)
+            suffix(y)
+            assert (x.out == y.out).all()
+            assert (x.pk.view(torch.int16) == y.pk.view(torch.int16)).all()
+            for b in range(y.B):
+                m = new[b] if ctx[b] >= 0 else 0
+                y.K[b] = torch.cat([y.K[b][:, :, : y.K[b].shape[2] - m], y.k[:, b, :m].transpose(1, 2)], 2)
+            check(y)
+        else:
+            suffix(x)
+            check(x)
+
+
 @pytest.mark.parametrize("hq,hkv,d,n,ctx", [
     (32, 8, 128, 70, [700, 64, 3]), (28, 4, 128, 128, [5000]), (8, 8, 64, 33, [1000, 2049, 0]), (40, 2, 128, 16, [300, 900]),
-    (8, 2, 64, 200, [4000]), (32, 8, 128, 128, [190] * 12), (4, 1, 128, 1, [6000, 77])])
+    (8, 2, 64, 200, [4000]), (32, 8, 128, 128, [190] * 12), (8, 2, 128, 9, [6000, 77])])
 @pytest.mark.parametrize("rope", [False, True])
 def test_suffix_bits_of_the_contiguous_call(hq, hkv, d, n, ctx, rope):
     for P in (16, 64, 512):
