@@ -10,6 +10,8 @@
 //    16; tiles, page numbers, K and V moves and the two-term probabilities as in page_decode.hip.
 //  * A row sees the keys up to its own token: the last tiles are masked per row, and a row that a wave's
 //    keys all lie past has no reference maximum there and adds nothing.
+//  * A probability of 0 times a value that is not finite is no 0: new tokens' values that are not finite
+//    are cleared in LDS, and added at the end to the rows that see them.
 //  * The new tokens' rows come from k_new / v_new (keys turned on load in the rope variant) and are stored
 //    into their pages by the workgroup whose range holds them.
 #include <type_traits>
@@ -176,11 +178,24 @@ page_few_kernel(PageFewArgs a) {
   }
   const bf16x2_t ones = __builtin_bit_cast(bf16x2_t, 0x3F803F80u);
 
+  bool odd = false;   // a value of the new tokens in this lane's pieces was not finite
   auto tile = [&](int k0, auto parity, u32x4 (&kcur)[2][KS], u32x4 (&knext)[2][KS]) {
     constexpr int P = decltype(parity)::value;
     const uint8_t* vcur = P ? v_lds1 : v_lds0;
     if (k0 + kTile < c1) load(k0 + kTile, knext, P ? v_lds0 : v_lds1);
     const bool fresh = k0 + kTile > ctx;   // the tile reaches the new tokens
+    if (fresh) {
+#pragma unroll
+      for (int i = 0; i < kTile / RPM; ++i) {   // (the pieces this lane moved)
+        const int key = min(min(k0 + (RPM * i & ~15), (c1 - 1) & ~15) + (RPM * i & 15) + ld_r, c1 - 1);
+        u32x4* piece = reinterpret_cast<u32x4*>(const_cast<uint8_t*>(vcur) + wave * kVTileBytes + RPM * i * kRowBytes + 16 * lane);
+        uint32_t w[4] = {(*piece)[0], (*piece)[1], (*piece)[2], (*piece)[3]};
+        if (key >= ctx && clear_odd(w)) {
+          *piece = u32x4{w[0], w[1], w[2], w[3]};
+          odd = true;
+        }
+      }
+    }
     if constexpr (kRope) {
       if (fresh) {   // their keys, read unrotated, turned to their positions
 #pragma unroll
@@ -265,6 +280,20 @@ page_few_kernel(PageFewArgs a) {
       tile(k0, std::integral_constant<int, 0>{}, k_a, k_b);
       if (k0 + kTile < c1) tile(k0 + kTile, std::integral_constant<int, 1>{}, k_b, k_a);
     }
+  }
+
+  if (__any(odd)) {   // those values, to the rows that see them
+    for (int key = max(c0, ctx); key < c1; ++key)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+        if (key <= qpos[nb])
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = bf16_to_f32(Vn[(key - ctx) * new_stride + 16 * db + 4 * g4 + e]);
+              if (!(fabsf(v) < INFINITY)) oacc[nb][db][e] += v;
+            }
   }
 
   // The new tokens of this range into their pages (nobody reads those rows from the pages in this launch).

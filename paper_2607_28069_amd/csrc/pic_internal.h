@@ -26,6 +26,21 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
 }
 
+// Of 8 packed bfloat16 values, those that are not finite set to 0; whether there were any.  (An
+// exponent of ones plus one carries into the sign's place.)
+__device__ __forceinline__ bool clear_odd(uint32_t (&w)[4]) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) any |= (w[i] & 0x7F807F80u) + 0x00800080u;
+  if ((any & 0x80008000u) == 0) return false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((w[i] & 0x7F80u) == 0x7F80u) w[i] &= 0xFFFF0000u;
+    if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] &= 0xFFFFu;
+  }
+  return true;
+}
+
 // ---- launchers (each returns hipSuccess or the launch error) ----
 
 hipError_t launch_rope_table(const double* inv_freq_host, int half, int32_t max_abs_delta,

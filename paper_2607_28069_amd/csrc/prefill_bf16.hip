@@ -249,6 +249,7 @@ prefill_bf16_kernel(PrefillArgs a) {
   __shared__ __attribute__((aligned(4096))) uint8_t v_lds1[kTileBytes];
   // paged and rope modes: each wave's cos/sin of the key rows it turns (4 KB per wave)
   __shared__ __attribute__((aligned(16))) uint8_t cs_lds[(kPool || kRope) ? kWaves * 4096 : 16];
+  __shared__ int odd_lds;   // pages modes: a value of the new tokens was not finite
   // paged mode: each wave's unturned Q^T operand (8 KB per wave), the source of every turn
   __shared__ __attribute__((aligned(16))) uint8_t q_lds[kPool ? kWaves * kQBytes : 16];
 
@@ -476,6 +477,7 @@ prefill_bf16_kernel(PrefillArgs a) {
     }
   }
   if (kPages && row0_wg >= M) return;   // (uniform) no query row: stored its share of the suffix only
+  if (kPages && tid == 0) odd_lds = 0;
   // row of q / out / a split's partials of this request's packed row r2 (token r2 / n_rep)
   auto row_at = [&](int r2, int tok2) {
     return (((int64_t)l * a.batch + b) * a.n_suffix + tok2) * a.n_q_heads + g * n_rep + (r2 - tok2 * n_rep);
@@ -792,6 +794,22 @@ prefill_bf16_kernel(PrefillArgs a) {
                                          pack_bf16x2(x2[4], x2[5]), pack_bf16x2(x2[6], x2[7])};
   };
   auto wait_loads = [&]() { __builtin_amdgcn_s_waitcnt(0x0F70); };   // vmcnt(0)
+  // Pages modes: a probability of 0 times a value that is not finite is no 0.  New tokens' values that are
+  // not finite are cleared in LDS, by the lane that moved them, before any wave reads the tile, and added
+  // at the end to the rows that see them.
+  auto clear_values = [&](uint8_t* vt, int t) {   // global tile t, landed in vt
+    if ((t + 1) * kKeys <= ctx) return;
+#pragma unroll
+    for (int i = 0; i < kLoadSteps; ++i) {
+      if (t * kKeys + kRowsPerLoad * kWaves * i + ld_row < ctx) continue;
+      u32x4* piece = reinterpret_cast<u32x4*>(vt + (kRowsPerLoad * kWaves * i + kRowsPerLoad * wave) * kRowBytes + 16 * lane);
+      uint32_t w[4] = {(*piece)[0], (*piece)[1], (*piece)[2], (*piece)[3]};
+      if (clear_odd(w)) {
+        *piece = u32x4{w[0], w[1], w[2], w[3]};
+        odd_lds = 1;
+      }
+    }
+  };
   // Rope mode: turn the suffix rows (keys ctx .. n_keys - 1) of K tile t, landed in `kt`, to
   // their positions; this lane's item is chunks rot_c and rot_c + C / 2 of row rot_row.
   auto rope_cs = [&](int t) {   // this lane's cos/sin for its suffix row of K tile t -> cos/sin area
@@ -1016,6 +1034,7 @@ prefill_bf16_kernel(PrefillArgs a) {
     }
   }
   __syncthreads();
+  if constexpr (kPages) clear_values(v_lds0, t0);   // (read after the next barrier)
   f32x16_t s_a[2], s_b[2];   // scores of the current / next tile, swapped every tile
   // local tiles [0, t_live) hold keys some row of this wave sees.  Outside table mode that is all of
   // them, or none for a wave whose rows are all past the last (a short suffix, a last m-tile):
@@ -1162,6 +1181,9 @@ prefill_bf16_kernel(PrefillArgs a) {
     if (t + 1 < n_tiles) finish_scores(t0 + t + 1, snext);
     }
     wait_loads();
+    if constexpr (kPages) {
+      if (t + 1 < n_tiles) clear_values(v_free, t0 + t + 1);
+    }
     if constexpr (kRope) {
       if (t + 2 < n_tiles && (t0 + t + 3) * kKeys > ctx) rope_own(k_free, t0 + t + 2);
     }
@@ -1203,6 +1225,18 @@ prefill_bf16_kernel(PrefillArgs a) {
 
   // ---- lane holds head dims 32 db + 8 qd + 4 hh + (0..3) of its row
   flush_pending();   // the last tile's last slice
+  if constexpr (kPages) {
+    if (odd_lds && row_ok) {
+      for (int key = max(t0 * kKeys, ctx); key < min((t0 + n_tiles) * kKeys, qpos + 1); ++key)
+#pragma unroll
+        for (int db = 0; db < kDB; ++db)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float v = bf16_to_f32(Vs[(key - ctx) * suf_stride + 32 * db + 8 * (e >> 2) + 4 * hh + (e & 3)]);
+            if (!(fabsf(v) < INFINITY)) oacc[db][e] += v;
+          }
+    }
+  }
   const float l_tot = pair_sum(l_part);
   const bool wave_rows = __any(row_ok);
   // (lane number as the epilogue sees it: opaque, so that what follows from it is worked out here

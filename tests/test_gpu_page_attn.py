@@ -288,3 +288,31 @@ def test_binding_refusals():
     assert (x.out == SENTINEL).all()
     decode(x)
     check(x, decoded=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d,n", [(32, 8, 128, 5), (8, 2, 64, 8), (8, 2, 128, 40), (32, 8, 128, 70), (4, 4, 64, 130)])
+@pytest.mark.parametrize("rope", [False, True])
+def test_suffix_values_that_are_not_finite(dtype, hq, hkv, d, n, rope):
+    """An infinity or NaN in a new token's value reaches the tokens that see it, in its head dim, and no other."""
+    if rope and dtype == "f32":
+        return
+    ctx, new = [70, 3000, 0, 64], [n, n, n - 1, n // 2]
+    x = setup(hq, hkv, d, dtype, 16, ctx, new, n=n)
+    y = setup(hq, hkv, d, dtype, 16, ctx, new, n=n)
+    bad = [(0, n - 1, 0, 3, math.inf), (1, n // 2, hkv - 1, d - 1, math.nan), (1, n - 1, 0, 0, -math.inf),
+           (2, n - 2, 0, 17, math.inf), (3, n // 2 - 1, 0, 40, math.nan)]
+    for b, i, g, c, v in bad:
+        x.v[0, b, i, g, c] = v
+    r = rope_table(x) if rope else None
+    suffix(x, rope=r)
+    suffix(y, rope=r)
+    rep, want = hq // hkv, y.out.clone()
+    for b, i, g, c, v in bad:
+        want[0, b, i: new[b], g * rep: (g + 1) * rep, c] = v
+    nan = torch.isnan(want)
+    assert (torch.isnan(x.out) == nan).all()
+    assert ((x.out == want) | nan).all() if dtype == "bf16" else torch.allclose(x.out[~nan], want[~nan], rtol=1e-5, atol=1e-6)
+    for b in range(4):   # the stored rows keep them
+        row = rows(x, b, ctx[b], ctx[b] + new[b])
+        assert torch.equal(x.pv[0][:, row].isfinite(), x.v[0, b, : new[b]].transpose(0, 1).isfinite())
