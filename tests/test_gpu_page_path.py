@@ -199,7 +199,7 @@ def _calls(x, out, ws):
                              out[1], ws[1])
     pic.pic_page_decode_attn(x["m"], x["pg"], x["q1"], x["k1"], x["v1"], x["pk"], x["pv"], x["table"], x["B"], x["len"], 0, x["mx"],
                              out[2], ws[2])
-    pic.pic_page_copy(x["m"], x["pg"], x["pk"], x["pv"], [[0, x["pg"].n_pages - 1]])
+    pic.pic_page_copy(x["m"], x["pg"], x["pk"], x["pv"], x["pairs"])
 
 
 def _state(seed, B=3, n=33, P=16, hq=16, hkv=4, d=128):
@@ -211,6 +211,8 @@ def _state(seed, B=3, n=33, P=16, hq=16, hkv=4, d=128):
     x = dict(m=s.model, pg=s.pages, q=s.q, k=s.k, v=s.v, pk=torch.nan_to_num(s.pk), pv=torch.nan_to_num(s.pv), table=s.table, B=B,
              len=s.len, mx=s.max_ctx, n=n, nv=s.n_valid, q3=f(2, B, 3, hq, d), k3=f(2, B, 3, hkv, d), v3=f(2, B, 3, hkv, d),
              q1=f(2, B, hq, d), k1=f(2, B, hkv, d), v1=f(2, B, hkv, d))
+    free = sorted(set(range(s.pages.n_pages)) - set(s.table_host.ravel().tolist()))
+    x["pairs"] = [[int(s.table_host[0, 0]), free[0]], [int(s.table_host[1, 1]), free[1]]]   # onto pages nobody reads
     out = [torch.zeros_like(x[i]) for i in ("q", "q3", "q1")]
     m = x["m"]
     ws = [torch.empty(max(b, 16), dtype=torch.uint8, device=DEV) for b in (
