@@ -478,13 +478,26 @@ def pic_page_blocks(pages: Pages, page_table, blocks) -> np.ndarray:
     return out[: n.value]
 
 
-def _same_device(*tensors):
-    """The launch goes to the current device: tensors of another one are refused."""
+def _on_device(tensors, stream):
+    """(addresses, stream handle) of a launch on the current device: dense tensors there (None -> NULL)."""
     import torch
     at = torch.cuda.current_device()
+    ptrs = []
     for t in tensors:
-        if t is not None and t.get_device() != at:
-            raise ValueError(f"tensor on device {t.get_device()}, the current one is {at}")
+        if t is None:
+            ptrs.append(None)
+            continue
+        if t.get_device() != at:   # (-1 for a host tensor)
+            raise ValueError("device buffer expected: got a host tensor" if not t.is_cuda else
+                             f"tensor on device {t.get_device()}, the current one is {at}")
+        if not t.is_contiguous():
+            raise ValueError("device buffer must be contiguous")
+        ptrs.append(t.data_ptr())
+    if stream is None:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (not a public name, see _stream)
+        if raw is not None:
+            return ptrs, raw(at)
+    return ptrs, _stream(stream)
 
 
 def pic_page_copy(model: Model, pages: Pages, pages_k, pages_v, pairs, stream=None):
@@ -492,57 +505,51 @@ def pic_page_copy(model: Model, pages: Pages, pages_k, pages_v, pairs, stream=No
     pairs, p_pairs = _host_i32(pairs)
     if pairs.size and (pairs.ndim != 2 or pairs.shape[1] != 2):
         raise ValueError("pairs: [n][2] expected")
-    k, v = _ptr(pages_k), _ptr(pages_v)
-    _same_device(pages_k, pages_v)
-    _check(load().pic_page_copy(ctypes.byref(model), ctypes.byref(pages), k, v, p_pairs, pairs.size // 2,
-                                _stream(stream)))
+    (k, v), st = _on_device((pages_k, pages_v), stream)
+    _check(load().pic_page_copy(ctypes.byref(model), ctypes.byref(pages), k, v, p_pairs, pairs.size // 2, st))
 
 
-def _page_args(model, pages, tensors, page_table, batch, lens):
-    """The leading arguments of the attention calls over pages."""
-    args = [_ptr(t) for t in tensors] + [_ptr(page_table), int(batch), _ptr(lens)]
-    _same_device(*tensors, page_table, lens)
-    return (ctypes.byref(model), ctypes.byref(pages), *args)
+def _ws_bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
 
 
 def pic_page_suffix_attn(model: Model, pages: Pages, q, k_suf, v_suf, pages_k, pages_v, page_table, batch, ctx_len,
                          max_ctx, n_suffix, out, workspace=None, n_valid=None, scale=0.0, stream=None):
     """page_table: device int32 [batch][table_cap]; n_valid: None, or device int32 [batch] tokens used."""
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    args = _page_args(model, pages, (q, k_suf, v_suf, pages_k, pages_v), page_table, batch, ctx_len)
-    _check(load().pic_page_suffix_attn(*args, int(max_ctx), _ptr(n_valid), int(n_suffix), float(scale), _ptr(out),
-                                       _ptr(workspace), ws_bytes, _stream(stream)))
+    (*a, tab, lens, nv, o, ws), st = _on_device((q, k_suf, v_suf, pages_k, pages_v, page_table, ctx_len, n_valid, out,
+                                                 workspace), stream)
+    _check(load().pic_page_suffix_attn(ctypes.byref(model), ctypes.byref(pages), *a, tab, int(batch), lens, int(max_ctx),
+                                       nv, int(n_suffix), float(scale), o, ws, _ws_bytes(workspace), st))
 
 
 def pic_page_suffix_attn_rope(model: Model, pages: Pages, q, k_suf, v_suf, pages_k, pages_v, page_table, batch, ctx_len,
                               max_ctx, n_suffix, table, max_abs_delta, out, workspace=None, n_valid=None, scale=0.0,
                               stream=None):
     """q / k_suf unrotated: turned to positions ctx_len[b] + i inside the kernel."""
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    args = _page_args(model, pages, (q, k_suf, v_suf, pages_k, pages_v), page_table, batch, ctx_len)
-    _check(load().pic_page_suffix_attn_rope(*args, int(max_ctx), _ptr(n_valid), int(n_suffix), _ptr(table),
-                                            int(max_abs_delta), float(scale), _ptr(out), _ptr(workspace), ws_bytes,
-                                            _stream(stream)))
+    (*a, tab, lens, nv, rt, o, ws), st = _on_device((q, k_suf, v_suf, pages_k, pages_v, page_table, ctx_len, n_valid, table,
+                                                     out, workspace), stream)
+    _check(load().pic_page_suffix_attn_rope(ctypes.byref(model), ctypes.byref(pages), *a, tab, int(batch), lens,
+                                            int(max_ctx), nv, int(n_suffix), rt, int(max_abs_delta), float(scale), o, ws,
+                                            _ws_bytes(workspace), st))
 
 
 def pic_page_decode_attn(model: Model, pages: Pages, q, k_new, v_new, pages_k, pages_v, page_table, batch, base_len,
                          step, max_base_len, out, workspace=None, n_splits=0, scale=0.0, stream=None):
     """page_table: device int32 [batch][table_cap]; a negative base_len marks padding of the batch."""
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    args = _page_args(model, pages, (q, k_new, v_new, pages_k, pages_v), page_table, batch, base_len)
-    _check(load().pic_page_decode_attn(*args, int(step), int(max_base_len), float(scale), int(n_splits), _ptr(out),
-                                       _ptr(workspace), ws_bytes, _stream(stream)))
+    (*a, tab, lens, o, ws), st = _on_device((q, k_new, v_new, pages_k, pages_v, page_table, base_len, out, workspace), stream)
+    _check(load().pic_page_decode_attn(ctypes.byref(model), ctypes.byref(pages), *a, tab, int(batch), lens, int(step),
+                                       int(max_base_len), float(scale), int(n_splits), o, ws, _ws_bytes(workspace), st))
 
 
 def pic_page_decode_attn_rope(model: Model, pages: Pages, q, k_new, v_new, pages_k, pages_v, page_table, batch,
                               base_len, step, max_base_len, table, max_abs_delta, out, workspace=None, n_splits=0,
                               scale=0.0, stream=None):
     """q / k_new unrotated: turned to position base_len[b] + step inside the kernel."""
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    args = _page_args(model, pages, (q, k_new, v_new, pages_k, pages_v), page_table, batch, base_len)
-    _check(load().pic_page_decode_attn_rope(*args, int(step), int(max_base_len), _ptr(table), int(max_abs_delta),
-                                            float(scale), int(n_splits), _ptr(out), _ptr(workspace), ws_bytes,
-                                            _stream(stream)))
+    (*a, tab, lens, rt, o, ws), st = _on_device((q, k_new, v_new, pages_k, pages_v, page_table, base_len, table, out,
+                                                 workspace), stream)
+    _check(load().pic_page_decode_attn_rope(ctypes.byref(model), ctypes.byref(pages), *a, tab, int(batch), lens, int(step),
+                                            int(max_base_len), rt, int(max_abs_delta), float(scale), int(n_splits), o, ws,
+                                            _ws_bytes(workspace), st))
 
 
 def pic_status_string(status: int) -> str:
