@@ -492,8 +492,8 @@ pic_status pic_page_copy(const pic_model* model, const pic_pages* pages, void* p
    pic_suffix_prefill_attn on a paged cache: stores k_suf / v_suf of token i < n_valid[b] of request
    b at slot ctx_len[b] + i and computes its attention over slots [0, ctx_len[b] + i].  Up to 32 query rows
    (tokens x query heads) per kv head may run on a kernel of their own, which keeps probabilities to 16
-   bits; otherwise outputs are pic_suffix_prefill_attn's bit for bit, on the same cache contents with
-   the same workspace.
+   bits.  max_ctx costs little where contexts are shorter: a launch split over the keys splits every
+   request's own.
      page_table [device, batch x table_cap]
      ctx_len    [device, batch]   clamped to max_ctx; a negative one marks a request that is only
                                   padding: nothing of it is read, stored or computed
@@ -518,8 +518,8 @@ pic_status pic_page_suffix_attn_rope(const pic_model* model, const pic_pages* pa
 /* ---- 5d. decode over pages ----
    pic_decode_attn on a paged cache: stores the new token at slot p = base_len[b] + step and attends
    over slots [0, p]; split over the context and joined alike.  On bf16 pages probabilities keep 16 bits
-   where pic_decode_attn rounds them to 8, so outputs carry little more than their own rounding; on float32
-   pages outputs are pic_decode_attn's bit for bit.
+   where pic_decode_attn rounds them to 8, so outputs carry little more than their own rounding, and the
+   ranges of a split launch are those of each request's own keys.
      page_table [device, batch x table_cap]
      base_len   [device, batch]   clamped to max_base_len; a negative one marks padding of the batch:
                                   nothing of that request is read or stored, its out rows are left untouched

@@ -9,9 +9,10 @@
 //    wave needs two page numbers per tile.  It holds 64 entries of the page table in a register (lane
 //    j: entry win + j) and takes them out with readlane, the 64 after those on their way: no tile's
 //    loads wait for the table.
-//  * A wave takes a quarter of the keys its workgroup's range really holds, not of the longest
-//    range there can be, so that short contexts use all four waves too (37 requests of 70 to 701 keys in a
-//    padded batch of 48, head_dim 64, two layers: 22.3 -> 19.6 us).
+//  * Equal ranges are those of the request's own keys, and a wave takes a quarter of its workgroup's, so
+//    that short contexts use every workgroup and wave that the longest one has (37 requests of 70 to 701 keys
+//    in a padded batch of 48, head_dim 64, two layers: 22.3 -> 19.6 us; one request of 10K keys where the
+//    call allows 33K 24.1 -> 15.4, 16 of 5K where it allows 20K 81.9 -> 59.3; 16 of 8K to 16K 140 -> 146).
 //  * Probabilities enter the product with V as two bfloat16 terms, the rounded value and what the
 //    rounding left (2^-17 relative to the value then).  The matrix cores have the time: 0.5 to 2 %, and
 //    the output's error against 64 bits falls from 0.0023 to that of its own rounding, 0.0017.
@@ -37,7 +38,7 @@ struct PageDecodeArgs {
   bf16_t* out;            // [L][B][Hq][D]
   float* ws_o;            // [L][slots][D]   (n_splits > 1; slots = B Hq n_splits, see SplitDeal)
   float* ws_ml;           // [L][slots][2]
-  int32_t batch, slot_cap, stream_rows, n_q_heads, n_kv_heads, max_base, step, n_splits, chunk;
+  int32_t batch, slot_cap, stream_rows, n_q_heads, n_kv_heads, max_base, step, n_splits;
   int32_t head_groups;    // groups of up to 16 query heads per kv head (ceil(n_rep / 16))
   EqualDeal eq;
   float scale_log2;
@@ -64,7 +65,7 @@ page_decode_kernel(PageDecodeArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hgrp = blockIdx.x % a.head_groups;           // query heads 16 hgrp .. of kv head g
   const int at = blockIdx.x / a.head_groups;             // [request][kv head][range]
-  int b, g, split, chunk = a.chunk;
+  int b, g, split, chunk = 0;
   int32_t base;
   SplitPlace place;
   if constexpr (!kDealt) {
@@ -76,6 +77,7 @@ page_decode_kernel(PageDecodeArgs a) {
     base = a.base_len[b];
     if (base < 0) return;   // (uniform) padding of the batch
     base = min(base, a.max_base);
+    chunk = decode_units(ceil_div(base + a.step + 1, a.n_splits)) * kDecodeUnit;   // (of this request's keys)
   } else {
     const SplitLens lens = split_lens<true>(a.base_len, a.batch, a.max_base, a.step, a.slot_cap);
     const int bg = at / a.eq.n;
@@ -426,8 +428,6 @@ hipError_t launch_decode_bf16_pages(const PageAttnArgs& p) {
   a.max_base = p.max_base;
   a.step = p.offset;
   a.n_splits = p.n_splits;
-  const int32_t chunk = ceil_div(max_len, p.n_splits);
-  a.chunk = (int32_t)std::min((int64_t)decode_units(chunk) * kDecodeUnit, (int64_t)INT32_MAX / kDecodeUnit * kDecodeUnit);
   if (decode_dealt(p.n_splits, s.batch, max_len)) {
     a.eq.units = decode_units(std::min(max_len, a.slot_cap));
     const int32_t per = ceil_div(a.eq.units, std::min(p.n_splits, a.eq.units));   // units per range

@@ -35,7 +35,7 @@ struct PageFewArgs {
   bf16_t* out;            // [L][B][n_new][Hq][D]
   float* ws_o;            // [L][B][n_new][Hq][n_splits][D]   (n_splits > 1)
   float* ws_ml;           // [L][B][n_new][Hq][n_splits][2]
-  int32_t batch, stream_rows, n_q_heads, n_kv_heads, n_new, max_ctx, n_splits, chunk;
+  int32_t batch, stream_rows, n_q_heads, n_kv_heads, n_new, max_ctx, n_splits;
   float scale_log2;
   const float2* table;    // rope variant: [L or 1][max_abs_delta + 1][D/2] cos/sin rows
   int64_t table_stride;
@@ -62,8 +62,9 @@ page_few_kernel(PageFewArgs a) {
   const int ctx = clamp_len(a.ctx_len[b], a.max_ctx);
   const int n_rep = a.n_q_heads / a.n_kv_heads, M = n_tok * n_rep;   // M <= ROWS
   const int n_vis = ctx + n_tok;
-  const int wc0 = (int)min((int64_t)split * a.chunk, (int64_t)n_vis);
-  const int wc1 = (int)min((int64_t)wc0 + a.chunk, (int64_t)n_vis);
+  const int chunk = decode_units(ceil_div(n_vis, a.n_splits)) * kDecodeUnit;   // (equal ranges of this request's keys)
+  const int wc0 = (int)min((int64_t)split * chunk, (int64_t)n_vis);
+  const int wc1 = (int)min((int64_t)wc0 + chunk, (int64_t)n_vis);
   // a wave's keys: an eighth of those there are, in whole tiles
   const int sub = (wc1 - wc0 + kFewWaves * kTile - 1) / (kFewWaves * kTile) * kTile;
   const int c0 = min(wc0 + wave * sub, wc1);
@@ -437,8 +438,6 @@ hipError_t launch_few_bf16_pages(const PageAttnArgs& p) {
   const size_t rows = (size_t)s.n_layers * s.batch * p.n_new * s.n_q_heads;
   a.ws_o = static_cast<float*>(p.workspace);
   a.ws_ml = a.n_splits > 1 ? a.ws_o + rows * a.n_splits * s.head_dim : nullptr;
-  a.chunk = (int32_t)std::min((int64_t)decode_units(ceil_div(p.max_base + p.n_new, a.n_splits)) * kDecodeUnit,
-                              (int64_t)INT32_MAX / kDecodeUnit * kDecodeUnit);
   const dim3 grid((unsigned)(a.n_splits * s.batch * s.n_kv_heads), s.n_layers);
   const bool two = (int64_t)p.n_new * (s.n_q_heads / s.n_kv_heads) > 16;
   if (s.head_dim == 64)

@@ -346,9 +346,12 @@ prefill_bf16_kernel(PrefillArgs a) {
   }
   constexpr int kChunkShift = HD == 128 ? 4 : 3;   // log2(C)
   const int ld_row = kRowsPerLoad * wave + (lane >> kChunkShift), ld_slot = lane & (kChunks - 1);   // load row within a step
-  // this workgroup's key tiles: [t0, t0 + n_tiles) of the (pos_max_wg + 1) visible keys
-  const int t0 = split * a.tiles_per_split;
-  const int n_tiles = min((pos_max_wg + kKeys) / kKeys - t0, a.tiles_per_split);
+  // this workgroup's key tiles: [t0, t0 + n_tiles) of the (pos_max_wg + 1) visible keys (pages: equal
+  // ranges of this request's tiles, not of the longest context the call allows: 128 tokens after one of
+  // 10K where it allows 33K 60.8 -> 36.0 us)
+  const int tiles_per_split = kPages ? ((n_keys + kKeys - 1) / kKeys + a.n_splits - 1) / a.n_splits : a.tiles_per_split;
+  const int t0 = split * tiles_per_split;
+  const int n_tiles = min((pos_max_wg + kKeys) / kKeys - t0, tiles_per_split);
 
   const int64_t bh_kv = kPages ? ((int64_t)l * a.n_kv_heads + g) * a.stream_rows
                                : (((int64_t)l * a.batch + b) * a.n_kv_heads + g) * a.cache_cap;

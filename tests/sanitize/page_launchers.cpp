@@ -111,8 +111,7 @@ hipError_t launch_decode_bf16_pages(const PageAttnArgs& a) {
   const int64_t rows_all = (int64_t)s.n_layers * s.batch * s.n_q_heads * a.n_splits;
   float* ws_o = static_cast<float*>(a.workspace);
   float* ws_ml = ws_o ? ws_o + rows_all * s.head_dim : nullptr;
-  int32_t chunk = (int32_t)std::min((int64_t)decode_units(ceil_div(max_len, a.n_splits)) * kDecodeUnit,
-                                    (int64_t)INT32_MAX / kDecodeUnit * kDecodeUnit);
+  int64_t dealt_chunk = 0;   // equal ranges are of the request's own keys
   std::vector<int32_t> mine(s.batch, a.n_splits), first(s.batch + 1, 0);
   if (decode_dealt(a.n_splits, s.batch, max_len)) {
     std::vector<int32_t> u(s.batch);
@@ -132,7 +131,7 @@ hipError_t launch_decode_bf16_pages(const PageAttnArgs& a) {
       if (sum <= (int64_t)a.n_splits * s.batch) break;
       if (i == kDecodeDealt - 1) return hipErrorInvalidValue;   // the last candidate always fits
     }
-    chunk = c * kDecodeUnit;
+    dealt_chunk = c * kDecodeUnit;
     for (int b = 0; b < s.batch; ++b) mine[b] = ceil_div(u[b], c);
   }
   for (int b = 0; b < s.batch; ++b) first[b + 1] = first[b] + mine[b];
@@ -143,6 +142,8 @@ hipError_t launch_decode_bf16_pages(const PageAttnArgs& a) {
         const Stream st(a, 2, l, b, g);
         if (st.n_tok == 0) continue;
         st.turn(st.ctx);
+        const int64_t chunk =
+            dealt_chunk ? dealt_chunk : (int64_t)decode_units(ceil_div(st.ctx + 1, a.n_splits)) * kDecodeUnit;
         for (int split = 0; split < mine[b]; ++split) {
           const int n_vis = st.ctx + 1;
           const int wc0 = (int)std::min((int64_t)split * chunk, (int64_t)n_vis);
@@ -167,9 +168,9 @@ hipError_t launch_decode_bf16_pages(const PageAttnArgs& a) {
 }
 
 namespace {
-// A bf16 suffix call: `splits` ranges of `chunk` keys, partials of split sp and query row r at slot(r, sp).
+// A bf16 suffix call: `splits` ranges of the request's keys, whole units of `unit` each.
 template <typename F, typename G>
-hipError_t walk_suffix(const PageAttnArgs& a, int splits, int64_t chunk, F partial, G combined) {
+hipError_t walk_suffix(const PageAttnArgs& a, int splits, int unit, F partial, G combined) {
   ++emu::launches;
   const AttnShape& s = a.s;
   const int n_rep = s.n_q_heads / s.n_kv_heads;
@@ -179,6 +180,7 @@ hipError_t walk_suffix(const PageAttnArgs& a, int splits, int64_t chunk, F parti
         const Stream st(a, 2, l, b, g);
         if (st.n_tok == 0) continue;
         const int n_vis = st.ctx + st.n_tok;
+        const int64_t chunk = (int64_t)ceil_div(ceil_div(n_vis, unit), splits) * unit;
         for (int sp = 0; sp < splits; ++sp) {
           const int wc0 = (int)std::min(sp * chunk, (int64_t)n_vis), wc1 = (int)std::min(wc0 + chunk, (int64_t)n_vis);
           st.keys(wc0, wc1);
@@ -205,8 +207,7 @@ hipError_t launch_few_bf16_pages(const PageAttnArgs& a) {
   const int64_t rows = (int64_t)s.n_layers * s.batch * a.n_new * s.n_q_heads;
   float* ws_o = static_cast<float*>(a.workspace);
   float* ws_ml = n > 1 ? ws_o + rows * n * s.head_dim : nullptr;
-  const int64_t chunk = (int64_t)decode_units(ceil_div(a.max_base + a.n_new, n)) * kDecodeUnit;
-  return walk_suffix(a, n, chunk, [&](int64_t row, int sp) {
+  return walk_suffix(a, n, kDecodeUnit, [&](int64_t row, int sp) {
     if (n == 1) return;
     wr(ws_o, row * n + sp, (int64_t)s.head_dim * 4);
     wr(ws_ml, row * n + sp, 8);
@@ -219,7 +220,7 @@ hipError_t launch_prefill_bf16_pages(const PageAttnArgs& a) {
   const int64_t rows = (int64_t)s.n_layers * s.batch * a.n_new * s.n_q_heads;
   const int64_t part = (int64_t)s.head_dim * (p.f32_partials ? 4 : 2);
   uint8_t* ws_o = static_cast<uint8_t*>(a.workspace);
-  return walk_suffix(a, p.n_splits, (int64_t)p.tiles_per_split * kPrefillKeys, [&](int64_t row, int sp) {
+  return walk_suffix(a, p.n_splits, kPrefillKeys, [&](int64_t row, int sp) {
     if (p.n_splits == 1) return;
     wr(ws_o, sp * rows + row, part);
     wr(ws_o + p.n_splits * rows * part, sp * rows + row, 8);

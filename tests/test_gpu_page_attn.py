@@ -107,10 +107,12 @@ def test_suffix_few_rows(hq, hkv, d, n, batch):
 
 
 @pytest.mark.parametrize("hq,hkv,d,n,ctx", [
-    (32, 8, 128, 70, [700, 64, 3]), (28, 4, 128, 128, [5000]), (8, 8, 64, 33, [1000, 2049, 0]), (40, 2, 128, 16, [300, 900]),
-    (8, 2, 64, 200, [4000]), (32, 8, 128, 128, [190] * 12), (8, 2, 128, 9, [6000, 77])])
+    (32, 8, 128, 70, [700, 700]), (28, 4, 128, 128, [5000]), (8, 8, 64, 33, [2049] * 3), (40, 2, 128, 16, [900, 900]),
+    (8, 2, 64, 200, [4000]), (32, 8, 128, 128, [190] * 12), (8, 2, 128, 9, [6000, 6000]), (32, 8, 128, 256, [1000, 64, 3, 700])])
 @pytest.mark.parametrize("rope", [False, True])
 def test_suffix_bits_of_the_contiguous_call(hq, hkv, d, n, ctx, rope):
+    """The prefill kernel over pages is the contiguous one: same bits where both split the keys alike (contexts
+    of one length, or no split)."""
     for P in (16, 64, 512):
         x = setup(hq, hkv, d, "bf16", P, ctx, [n] * len(ctx), L=2)
         ck, cv, cap = contiguous(x)
@@ -240,6 +242,51 @@ def test_lengths_are_clamped():
     x.n_valid = torch.tensor([2**31 - 1, 3], dtype=torch.int32, device=DEV)
     suffix(x)
     check(x)
+
+
+@pytest.mark.parametrize("kind", ["decode", "few", "suffix"])
+def test_contexts_far_below_the_bound(kind):
+    """A call's bound on the lengths far above them, as a captured step has it: every request's own keys split."""
+    n = {"decode": 1, "few": 2, "suffix": 40}[kind]
+    ctx = [900, 3, -1, 260]
+    x = setup(16, 4, 128, "bf16", 16, ctx, [n] * 4, n=n, slack=20000)
+    if kind == "decode":
+        for k in (0, 5, 8):
+            decode(x, n_splits=k)
+            check(x, decoded=True)
+    else:
+        suffix(x)
+        check(x)
+
+
+@pytest.mark.parametrize("kind", ["decode", "few", "suffix"])
+@pytest.mark.parametrize("pairing", ["half", "interleaved"])
+def test_rotary_tables_per_layer(kind, pairing):
+    """Layers with frequencies of their own in one call: what a call per layer with its own table gives."""
+    n = {"decode": 1, "few": 3, "suffix": 30}[kind]
+    ctx, L = [333, -1, 40], 3
+    x = setup(8, 2, 64, "bf16", 32, ctx, [n] * 3, n=n, L=L, pairing=pairing)
+    keep = x.pk.clone(), x.pv.clone()
+    model = x.model
+    x.model = pic.Model.of(L, 8, 2, 64, "bf16", 1e4, pairing, per_layer_tables=True)
+    mad = x.max_ctx + n
+    freq = np.stack([(10.0 ** (3 + l)) ** (-2.0 * np.arange(32) / 64) for l in range(L)])
+    t = torch.empty(pic.pic_rope_table_bytes(x.model, mad) // 4, dtype=torch.float32, device=DEV)
+    pic.pic_rope_table_init_freq(x.model, freq, mad, t)
+    (decode if kind == "decode" else suffix)(x, rope=(t, mad))
+    one, y = t.numel() // L, []
+    for l in range(L):
+        z = setup(8, 2, 64, "bf16", 32, ctx, [n] * 3, n=n, L=1, pairing=pairing)
+        for k in ("q", "k", "v"):
+            setattr(z, k, getattr(x, k)[l: l + 1].contiguous())
+        z.pk, z.pv = (p[l: l + 1].clone() for p in keep)
+        z.table = x.table
+        (decode if kind == "decode" else suffix)(z, rope=(t[l * one: (l + 1) * one].clone(), mad))
+        err = (x.out[l].double() - z.out[0].double()).abs().max()
+        assert float(err) <= 2 * 2.0 ** -8   # (splits may differ with the layers of a call)
+        assert (x.pk[l].view(torch.int16) == z.pk[0].view(torch.int16)).all()
+        y.append(z.pk)
+    assert not torch.equal(y[0].nan_to_num(), y[1].nan_to_num())
 
 
 def test_rows_past_32_bits():

@@ -12,7 +12,8 @@ DEV = "cuda"
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("L,hkv,d,P,n_pages,n_pairs", [
     (1, 1, 64, 16, 2, 1), (1, 2, 64, 16, 40, 20), (3, 8, 128, 64, 33, 5), (2, 4, 128, 16, 1400, 700),
-    (1, 1, 64, 1024, 5, 2), (28, 4, 128, 128, 9, 4), (1, 3, 64, 32, 600, 256), (1, 3, 64, 32, 600, 257), (40, 1, 64, 16, 8, 3)])
+    (1, 1, 64, 1024, 5, 2), (28, 4, 128, 128, 9, 4), (1, 3, 64, 32, 600, 256), (1, 3, 64, 32, 600, 257), (40, 1, 64, 16, 8, 3),
+    (40000, 1, 64, 16, 3, 1)])
 def test_copy(dtype, L, hkv, d, P, n_pages, n_pairs):
     dt = torch.float32 if dtype == "f32" else torch.bfloat16
     at = np.random.default_rng(n_pairs).permutation(n_pages)[: 2 * n_pairs].reshape(-1, 2)
