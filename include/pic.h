@@ -499,7 +499,7 @@ pic_status pic_page_copy(const pic_model* model, const pic_pages* pages, void* p
                                   padding: nothing of it is read, stored or computed
      n_valid    [device, batch]   tokens used per request, clamped to [0, n_suffix]; the others are neither
                                   stored nor computed, their out rows left untouched.  NULL: all
-     max_ctx + n_suffix <= table_cap * page_tokens (PIC_ERR_CAPACITY)
+     max_ctx + n_suffix <= table_cap * page_tokens and <= 2^30 (PIC_ERR_CAPACITY)
      (q, k_suf, v_suf, out, scale and the workspace as for pic_suffix_prefill_attn; bf16 pages:
      n_pages * page_tokens and n_suffix * Hkv below 2^24)
    pic_page_suffix_attn_rope: q and k_suf unrotated, as for pic_suffix_prefill_attn_rope.  bf16 only. */
@@ -523,7 +523,7 @@ pic_status pic_page_suffix_attn_rope(const pic_model* model, const pic_pages* pa
      page_table [device, batch x table_cap]
      base_len   [device, batch]   clamped to max_base_len; a negative one marks padding of the batch:
                                   nothing of that request is read or stored, its out rows are left untouched
-     max_base_len + step + 1 <= table_cap * page_tokens (PIC_ERR_CAPACITY)
+     max_base_len + step + 1 <= table_cap * page_tokens and <= 2^30 (PIC_ERR_CAPACITY)
      (the other arguments and the workspace as for pic_decode_attn)
    pic_page_decode_attn_rope: q and k_new unrotated, as for pic_decode_attn_rope.  bf16 only. */
 pic_status pic_page_decode_attn(const pic_model* model, const pic_pages* pages, const void* q,

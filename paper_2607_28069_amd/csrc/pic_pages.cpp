@@ -15,6 +15,9 @@ using namespace pic;
 
 namespace {
 
+// Slots of a request that attention reads: positions rounded up to a workgroup's tile stay in 31 bits.
+constexpr int64_t kMaxSlots = int64_t(1) << 30;
+
 int page_shift(int32_t page_tokens) { return __builtin_ctz((unsigned)page_tokens); }
 
 pic_status check_pages(const pic_pages* pg) {
@@ -343,7 +346,8 @@ pic_status page_attn(const pic_model* model, const pic_pages* pages, const void*
     return fail(PIC_ERR_INVALID_ARG, "negative size");
   if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(PIC_ERR_INVALID_ARG, "scale must be finite and >= 0");
   const int64_t max_len = (int64_t)max_base + offset + n_new;
-  if (max_len > (int64_t)pages->table_cap * pages->page_tokens || max_len > INT32_MAX)
+  if (max_len > kMaxSlots) return fail(PIC_ERR_CAPACITY, "%lld slots per request (at most 2^30)", (long long)max_len);
+  if (max_len > (int64_t)pages->table_cap * pages->page_tokens)
     return fail(PIC_ERR_CAPACITY, "%lld slots per request exceed a page table of %d pages of %d tokens", (long long)max_len,
                 pages->table_cap, pages->page_tokens);
   if (rope && (max_abs_delta < 0 || max_abs_delta > kMaxAbsDelta || max_len - 1 > max_abs_delta))

@@ -302,6 +302,16 @@ def test_attention_refusals(p, name):
         assert call(pages=G.of(1 << 20, 16, 4)) == UNSUPPORTED   # a stream of 2^24 rows
 
 
+@pytest.mark.parametrize("name", NAMES)
+def test_attention_refuses_requests_past_2_30_slots(p, name):
+    """Tables that name pages more than once can hold positions past those the pages have."""
+    wide = pic.Pages.of(8, 1024, 1 << 21)
+    assert _attn(p, name=name, pages=wide, max=2**30, batch=0) == CAPACITY
+    assert _attn(p, name=name, pages=wide, max=2**31 - 1, batch=0) == CAPACITY
+    at_limit = _attn(p, name=name, pages=wide, max=2**30 - 8, batch=0)
+    assert at_limit == (RANGE if "rope" in name else 0)   # rope: no table is that long
+
+
 def test_copy_refusals(p):
     m, g = pic.Model.of(1, 4, 2, 64, "bf16", 1e4), pic.Pages.of(8, 16, 0)
 
