@@ -493,7 +493,8 @@ pic_status pic_page_copy(const pic_model* model, const pic_pages* pages, void* p
    b at slot ctx_len[b] + i and computes its attention over slots [0, ctx_len[b] + i].  Up to 32 query rows
    (tokens x query heads) per kv head may run on a kernel of their own, which keeps probabilities to 16
    bits.  max_ctx costs little where contexts are shorter: a launch split over the keys splits every
-   request's own.
+   request's own, long requests into more ranges than short ones where that ends the launch earlier (of
+   up to 64 requests), so the last bits of an output may depend on the lengths of the other requests.
      page_table [device, batch x table_cap]
      ctx_len    [device, batch]   clamped to max_ctx; a negative one marks a request that is only
                                   padding: nothing of it is read, stored or computed

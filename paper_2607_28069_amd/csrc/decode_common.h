@@ -66,12 +66,6 @@ struct SplitLens {
 struct SplitPlace {
   int32_t n, first;   // ranges of the request; those of the requests before it
 };
-// ceil(u / c) for 0 <= u < 2^24, 1 <= c, inv ~ 1 / c: a float32 quotient, off by one at most, put right
-__device__ __forceinline__ int32_t ceil_div24(int32_t u, int32_t c, float inv) {
-  int32_t q = (int32_t)((float)u * inv);
-  const int32_t r = u - q * c;
-  return q + (r > 0 ? 1 : 0) + (r > c ? 1 : 0) - (r <= -c ? 1 : 0);
-}
 // kPages: a negative length is padding of the batch and gets no range
 template <bool kPages>
 __device__ __forceinline__ SplitLens split_lens(const int32_t* base_len, int32_t batch, int32_t max_base, int32_t step,

@@ -146,4 +146,34 @@ PIC_HD RangeCandidates decode_range_candidates(int32_t units_total, int32_t unit
   return r;
 }
 
+// ---- Split prefill over pages: the key ranges of uneven requests ----
+// A split launch has n_splits workgroups per (request, kv head, tile of query rows).  Request b with u_b key
+// tiles, t_b used tokens and m_b tiles of query rows gets ceil(u_b / c) equal ranges, c the smallest size for
+// which workgroups (sum of m_b ceil(u_b / c)) and partials (of t_b ceil(u_b / c)) fit in those of n_splits ranges
+// of every request.  Candidates as above, from the mean, of 8 tiles at least (the combine reads a row's
+// partials one after another), up to what always fits; and where that is not enough shorter than the
+// longest request's share, every request gets n_splits ranges.  Equal shares / dealt, us, by c of that
+// share's tiles: 5 of 2K to 4K keys x 1 to 67 tokens (head_dim 64) 15 of 23 37.6 / 30.8; 6 of 15K to 33K x 100
+// (28 heads over 4) 74 of 103 260 / 207; 8 of 5K to 10K x 64 33 of 41 96 / 92.  Shorter by less than an eighth
+// or 4 tiles is not worth the 1.5 us that the combine's longer rows cost (4 of 7K to 10K x 32, 19 of 21, 45.3 /
+// 47.2); finding that out costs 1 us where lengths differ, and nothing that shows where they are equal.
+PIC_HD bool suffix_dealt(int32_t n_splits, int32_t batch) { return n_splits >= 2 && batch >= 2 && batch <= kDecodeDealt; }
+PIC_HD bool suffix_deal_pays(int32_t size, int32_t top) { return size + 4 <= top && size <= top - top / 8; }
+// tiles_total: sum of m_b u_b;  groups: batch * (tiles of the longest request's query rows)
+PIC_HD RangeCandidates suffix_range_candidates(int64_t tiles_total, int32_t tiles_longest, int32_t n_splits, int32_t groups) {
+  RangeCandidates r;
+  r.top = ceil_div(tiles_longest, n_splits < tiles_longest ? n_splits : tiles_longest);
+  const int64_t wgs = (int64_t)n_splits * groups;
+  const int32_t mean = (int32_t)((tiles_total + wgs - 1) / wgs), least = r.top < 8 ? r.top : 8;
+  r.lo = mean > least ? mean : least;
+  r.step = ceil_div(r.top > r.lo ? r.top - r.lo : 1, kDecodeDealt - 1);
+  return r;
+}
+// ceil(u / c) for 0 <= u <= 2^24, 1 <= c, inv ~ 1 / c: a float32 quotient, off by one at most, put right
+PIC_HD int32_t ceil_div24(int32_t u, int32_t c, float inv) {
+  int32_t q = (int32_t)((float)u * inv);
+  const int32_t r = u - q * c;
+  return q + (r > 0 ? 1 : 0) + (r > c ? 1 : 0) - (r <= -c ? 1 : 0);
+}
+
 }  // namespace pic

@@ -178,6 +178,8 @@ struct PrefillArgs {
   float scale_log2;
   PageMap map;              // pages modes: cache_k / cache_v are [L][Hkv][stream_rows][D]
   int32_t stream_rows;
+  bool may_deal;            // pages modes: key ranges dealt by length where that pays (deal_pages); ws_o and
+                            // ws_ml then hold [L][n_splits * batch * n_suffix * Hq], request after request
 };
 
 // Rope mode = suffix mode with the suffix queries and keys given unrotated: the kernel turns
@@ -226,6 +228,52 @@ __device__ __forceinline__ void rot_chunks(float (&x1)[8], float (&x2)[8], const
   }
 }
 
+// Key ranges of a split launch over pages, dealt to the requests by length where that pays
+// (suffix_range_candidates): the same in every wave of a launch and of its combine.
+struct PageDeal {
+  bool dealt;           // else n_splits ranges of every request
+  int32_t n, tok, ctx;  // lane b: request b's ranges (dealt), used tokens and context
+};
+__device__ __forceinline__ int32_t row_tiles(int32_t tok, int32_t n_rep) { return (tok * n_rep + kRowsPerWG - 1) / kRowsPerWG; }
+__device__ __forceinline__ PageDeal deal_pages(const int32_t* ctx_len, const int32_t* n_valid, int32_t batch, int32_t n_new,
+                                               int32_t max_ctx, int32_t n_rep, int32_t n_splits, int32_t m_tiles) {
+  const int lane = threadIdx.x & 63;
+  PageDeal d = {false, 0, 0, 0};
+  int32_t u = 0;   // lane b: key tiles of request b
+  if (lane < batch) {
+    const int32_t len = ctx_len[lane], used = n_valid ? n_valid[lane] : n_new;
+    d.tok = len < 0 ? 0 : clamp_len(used, n_new);
+    d.ctx = clamp_len(len, max_ctx);
+    if (d.tok > 0) u = (d.ctx + d.tok + kKeys - 1) / kKeys;
+  }
+  const int32_t u0 = __builtin_amdgcn_readfirstlane(u);
+  if (__ballot(lane < batch && (u != u0 || d.tok != n_new)) == 0) return d;
+  const int32_t m = row_tiles(d.tok, n_rep);
+  int64_t total = 0;
+  int32_t longest = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int32_t ub = __builtin_amdgcn_readlane(u, b);
+    total += (int64_t)ub * __builtin_amdgcn_readlane(m, b);
+    longest = max(longest, ub);
+  }
+  if (longest == 0) return d;
+  const RangeCandidates rc = suffix_range_candidates(total, longest, n_splits, batch * m_tiles);
+  if (!suffix_deal_pays(rc.lo, rc.top)) return d;
+  const int32_t c = rc.at(lane);   // lane i weighs candidate i
+  const float inv = __builtin_amdgcn_rcpf((float)c);
+  int32_t wgs = 0, parts = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int32_t nb = ceil_div24(__builtin_amdgcn_readlane(u, b), c, inv);
+    wgs += nb * __builtin_amdgcn_readlane(m, b);
+    parts += nb * __builtin_amdgcn_readlane(d.tok, b);
+  }
+  const uint64_t fits = __ballot(wgs <= n_splits * batch * m_tiles && parts <= n_splits * batch * n_new);   // (lane 63: always)
+  const int32_t size = __builtin_amdgcn_readlane(c, __ffsll((unsigned long long)fits) - 1);
+  d.dealt = suffix_deal_pays(size, rc.top);
+  d.n = ceil_div24(u, size, __builtin_amdgcn_rcpf((float)size));
+  return d;
+}
+
 template <int HD, int kMode, bool kInterleaved>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 prefill_bf16_kernel(PrefillArgs a) {
@@ -249,7 +297,9 @@ prefill_bf16_kernel(PrefillArgs a) {
   __shared__ __attribute__((aligned(4096))) uint8_t v_lds1[kTileBytes];
   // paged and rope modes: each wave's cos/sin of the key rows it turns (4 KB per wave)
   __shared__ __attribute__((aligned(16))) uint8_t cs_lds[(kPool || kRope) ? kWaves * 4096 : 16];
-  __shared__ int odd_lds;   // pages modes: a value of the new tokens was not finite
+  __shared__ int odd_lds;        // pages modes: a value of the new tokens was not finite
+  __shared__ int64_t part_lds;   // pages modes, through the key loop: part0
+  __shared__ int ranges_lds;     // and n_ranges
   // paged mode: each wave's unturned Q^T operand (8 KB per wave), the source of every turn
   __shared__ __attribute__((aligned(16))) uint8_t q_lds[kPool ? kWaves * kQBytes : 16];
 
@@ -258,7 +308,7 @@ prefill_bf16_kernel(PrefillArgs a) {
   const int per_xcd = (a.n_wg + kNumXcd - 1) / kNumXcd;
   const int w = blockIdx.x, at = w / kNumXcd;
   const int logical = (w % kNumXcd) * per_xcd + at;
-  if (logical >= a.n_wg) return;
+  if (!kPages && logical >= a.n_wg) return;   // (pages: below)
   // m-tiles of one (request, kv head) are dispatched one after another (so they stream its
   // keys concurrently, sharing the XCD's L2), the last one first: later query rows see more
   // keys, so the longest workgroups start earliest and short ones fill the end of the launch
@@ -274,16 +324,51 @@ prefill_bf16_kernel(PrefillArgs a) {
       bg = (logical - at + head) / a.m_tiles + (at - head) % a.tail_bgs;
     }
   }
-  const int b = bg / a.n_kv_heads, g = bg % a.n_kv_heads;
+  int b = bg / a.n_kv_heads, g = bg % a.n_kv_heads;
   const int l = blockIdx.y;
+  // pages: tokens of this request and its context; its key ranges and tiles of query rows; dealt: (tokens of)
+  // partials of the requests before it, else -1
+  int n_tok_b = 0, ctx_b = 0, n_ranges = a.n_splits, m_tiles_b = a.m_tiles, first = -1;
+  if constexpr (kPages) {
+    PageDeal d = {};
+    if (a.may_deal)
+      d = deal_pages(a.ctx_len, a.n_valid, a.batch, a.n_suffix, a.max_ctx, a.n_rep, a.n_splits, a.m_tiles);
+    if (d.dealt) {
+      const int32_t m = row_tiles(d.tok, a.n_rep), wgs = d.n * m * a.n_kv_heads;   // lane b: workgroups of request b
+      int total = 0;
+      for (int i = 0; i < a.batch; ++i) total += __builtin_amdgcn_readlane(wgs, i);
+      const int per = (total + kNumXcd - 1) / kNumXcd;
+      int in_b = (w % kNumXcd) * per + at;   // (per <= per_xcd)
+      if (at >= per || in_b >= total) return;
+      first = 0;
+      for (b = 0; in_b >= __builtin_amdgcn_readlane(wgs, b); ++b) {
+        in_b -= __builtin_amdgcn_readlane(wgs, b);
+        first += __builtin_amdgcn_readlane(d.n, b) * __builtin_amdgcn_readlane(d.tok, b);
+      }
+      n_ranges = __builtin_amdgcn_readlane(d.n, b);
+      m_tiles_b = __builtin_amdgcn_readlane(m, b);
+      mt = m_tiles_b - 1 - in_b % m_tiles_b;
+      split = (in_b / m_tiles_b) % n_ranges;
+      g = in_b / (m_tiles_b * n_ranges);
+    } else if (logical >= a.n_wg) {
+      return;
+    }
+    if (a.may_deal) {
+      n_tok_b = __builtin_amdgcn_readlane(d.tok, b);
+      ctx_b = __builtin_amdgcn_readlane(d.ctx, b);
+    } else {
+      n_tok_b = page_new_tokens(a.ctx_len, a.n_valid, b, a.n_suffix);
+      ctx_b = clamp_len(a.ctx_len[b], a.max_ctx);
+    }
+    if (n_tok_b == 0) return;   // (uniform) padding of the batch
+  }
 
   // (divisions by n_rep as multiply-highs: uniform operands then stay in scalar registers,
   // and with them every tile count, mask decision and load path derived from them)
   const int n_rep = a.n_rep;
   auto div_rep = [&](int x) { return (int)(((uint64_t)(uint32_t)x * a.rep_magic) >> 32); };
   // tokens of this request (pages modes: the used ones)
-  const int n_tok = kPages ? page_new_tokens(a.ctx_len, a.n_valid, b, a.n_suffix) : a.n_suffix;
-  if (kPages && n_tok == 0) return;   // (uniform) padding of the batch
+  const int n_tok = kPages ? n_tok_b : a.n_suffix;
   const int M = n_tok * n_rep;
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -298,7 +383,7 @@ prefill_bf16_kernel(PrefillArgs a) {
   // pos_min_wg / pos_max_wg: nearest / furthest position of this workgroup's query rows
   int ctx, qpos, pos_min_wg, pos_max_wg, nv_wg = 0;   // nv_wg: table mode, the request's used tokens
   if constexpr (!kTable) {
-    ctx = clamp_len(a.ctx_len[b], a.max_ctx);
+    ctx = kPages ? ctx_b : clamp_len(a.ctx_len[b], a.max_ctx);
     pos_min_wg = ctx + div_rep(row0_wg);
     pos_max_wg = ctx + div_rep(min(row0_wg + kRowsPerWG, M) - 1);
     qpos = ctx + tok;
@@ -349,7 +434,7 @@ prefill_bf16_kernel(PrefillArgs a) {
   // this workgroup's key tiles: [t0, t0 + n_tiles) of the (pos_max_wg + 1) visible keys (pages: equal
   // ranges of this request's tiles, not of the longest context the call allows: 128 tokens after one of
   // 10K where it allows 33K 60.8 -> 36.0 us)
-  const int tiles_per_split = kPages ? ((n_keys + kKeys - 1) / kKeys + a.n_splits - 1) / a.n_splits : a.tiles_per_split;
+  const int tiles_per_split = kPages ? ((n_keys + kKeys - 1) / kKeys + n_ranges - 1) / n_ranges : a.tiles_per_split;
   const int t0 = split * tiles_per_split;
   const int n_tiles = min((pos_max_wg + kKeys) / kKeys - t0, tiles_per_split);
 
@@ -365,7 +450,7 @@ prefill_bf16_kernel(PrefillArgs a) {
   // Cache assembly: the suffix rows go into slots [ctx, ctx + n_suffix), shared out over the
   // (request, kv head)'s workgroups (every m-tile and split stores a contiguous share of the
   // rows), so no workgroup carries the whole store ahead of its key loop.
-  const int asm_parts = a.m_tiles * a.n_splits, asm_part = split * a.m_tiles + mt;
+  const int asm_parts = m_tiles_b * n_ranges, asm_part = split * m_tiles_b + mt;
   const int asm_per = (n_tok + asm_parts - 1) / asm_parts;
   const int asm_i0 = min(asm_part * asm_per, n_tok), asm_i1 = min(asm_i0 + asm_per, n_tok);
   // pages: lane j holds where page table entry pwin + j lies in a stream, in bytes, and entry pwin + 56 + j
@@ -480,13 +565,26 @@ prefill_bf16_kernel(PrefillArgs a) {
     }
   }
   if (kPages && row0_wg >= M) return;   // (uniform) no query row: stored its share of the suffix only
-  if (kPages && tid == 0) odd_lds = 0;
+  // this range's partial of row 0 of q / out (a row of another request or layer, dealt: not one of this launch's)
+  int64_t part = 0;
+  auto part0 = [&]() -> int64_t { return kPages ? part : split * a.rows_total; };
+  if constexpr (kPages) {
+    part = split * a.rows_total;
+    if (first >= 0)
+      part = ((int64_t)l * a.batch * a.n_suffix * (a.n_splits - 1) + (first + (int64_t)split * n_tok) -
+               (int64_t)b * a.n_suffix) * a.n_q_heads;
+    if (tid == 0) {
+      odd_lds = 0;
+      part_lds = part;
+      ranges_lds = n_ranges;
+    }
+  }
   // row of q / out / a split's partials of this request's packed row r2 (token r2 / n_rep)
   auto row_at = [&](int r2, int tok2) {
     return (((int64_t)l * a.batch + b) * a.n_suffix + tok2) * a.n_q_heads + g * n_rep + (r2 - tok2 * n_rep);
   };
   if (n_tiles <= 0) {   // (uniform) a split past this workgroup's last visible key
-    if (a.n_splits > 1 && row_ok && hh == 0) a.ws_ml[split * a.rows_total + row_at(r, tok)] = make_float2(-INFINITY, 0.f);
+    if (n_ranges > 1 && row_ok && hh == 0) a.ws_ml[part0() + row_at(r, tok)] = make_float2(-INFINITY, 0.f);
     return;
   }
 
@@ -1240,6 +1338,10 @@ prefill_bf16_kernel(PrefillArgs a) {
           }
     }
   }
+  if constexpr (kPages) {
+    part = part_lds;
+    n_ranges = __builtin_amdgcn_readfirstlane(ranges_lds);
+  }
   const float l_tot = pair_sum(l_part);
   const bool wave_rows = __any(row_ok);
   // (lane number as the epilogue sees it: opaque, so that what follows from it is worked out here
@@ -1247,9 +1349,9 @@ prefill_bf16_kernel(PrefillArgs a) {
   int lane_e = lane;
   asm volatile("" : "+v"(lane_e));
   const int n_e = lane_e & 31, hh_e = lane_e >> 5;
-  if (a.n_splits > 1 && hh_e == 0 && row_ok) {
+  if (n_ranges > 1 && hh_e == 0 && row_ok) {
     const int r2 = row0_wg + wave * kRowsPerWave + n_e;
-    a.ws_ml[split * a.rows_total + row_at(r2, div_rep(r2))] = make_float2(m_run, l_tot);
+    a.ws_ml[part0() + row_at(r2, div_rep(r2))] = make_float2(m_run, l_tot);
   }
   if (!wave_rows) return;
   // Normalised: the output in bf16, or one split's share of it in bf16 or float32 (with its
@@ -1297,8 +1399,8 @@ prefill_bf16_kernel(PrefillArgs a) {
       if (ok) *reinterpret_cast<u32x4*>(base + row_at(r2, tok2) * stride + off + 16 * c) = x;
     }
   };
-  if (a.n_splits > 1 && a.f32_partials) {
-    uint8_t* base = static_cast<uint8_t*>(a.ws_o) + split * a.rows_total * (4 * kHD);
+  if (n_ranges > 1 && a.f32_partials) {
+    uint8_t* base = static_cast<uint8_t*>(a.ws_o) + part0() * (4 * kHD);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {   // a row of the stage holds half a float32 row
 #pragma unroll
@@ -1324,8 +1426,8 @@ prefill_bf16_kernel(PrefillArgs a) {
         *reinterpret_cast<uint2*>(stage + chunk_at(n_e, 4 * db + qd) + 8 * hh_e) = v;
       }
     wave_sync();
-    if (a.n_splits == 1) flush_rows(reinterpret_cast<uint8_t*>(a.out), kRowBytes, 0);
-    else flush_rows(static_cast<uint8_t*>(a.ws_o) + split * a.rows_total * kRowBytes, kRowBytes, 0);
+    if (n_ranges == 1) flush_rows(reinterpret_cast<uint8_t*>(a.out), kRowBytes, 0);
+    else flush_rows(static_cast<uint8_t*>(a.ws_o) + part0() * kRowBytes, kRowBytes, 0);
   }
 }
 
@@ -1335,24 +1437,54 @@ prefill_bf16_kernel(PrefillArgs a) {
 // 2 D threads: D / 8 lanes per row, 8 head dims per lane; every split's loads are issued without a branch
 // between them (a split that saw no key of the row, reference max -inf, is dropped by a
 // select: its sums are not finite).  With n_valid (table and pages modes), rows of tokens past
-// n_valid[b] are left untouched.
+// n_valid[b] are left untouched.  kDealt (pages modes): ranges may be dealt by
+// length; grid (n_q Hq / 16, L B), so that a workgroup has one request's.
 // kBatch: splits whose loads are issued together (4, 8 or 16, the smallest that covers n_splits:
 // a larger batch holds more registers and lowers the occupancy that few splits need)
 constexpr int kCombineRowsPerWG = 16;
-template <int HD, int kCombineBatch, typename PT>
+template <int HD, int kCombineBatch, typename PT, bool kDealt>
 __global__ void __launch_bounds__(256) prefill_combine_kernel(const PT* __restrict__ ws_o,
                                                               const float2* __restrict__ ws_ml,
                                                               int32_t n_splits, int64_t rows_total,
                                                               const int32_t* __restrict__ n_valid,
                                                               const int32_t* __restrict__ lens,
                                                               int32_t n_q, int32_t n_q_heads,
-                                                              int32_t batch,
-                                                              bf16_t* __restrict__ out) {
+                                                              int32_t batch, int32_t max_ctx, int32_t n_rep,
+                                                              int32_t m_tiles, bf16_t* __restrict__ out) {
   constexpr int kLanes = HD / 8;   // lanes per row
   constexpr int kPieces = sizeof(PT) / 2;   // 16-byte pieces of a lane's 8 head dims
-  const int64_t row = (int64_t)blockIdx.x * kCombineRowsPerWG + threadIdx.x / kLanes;
+  int64_t row = (int64_t)blockIdx.x * kCombineRowsPerWG + threadIdx.x / kLanes;
+  int64_t part = row, stride = rows_total;   // a row's partials: the first one's place, from one to the next
+  if constexpr (kDealt) {
+    // (one wave deals for all four: thousands of workgroups do, and the sum of it counts)
+    __shared__ int32_t n_lds, tok_lds, first_lds;   // (first_lds -1: not dealt)
+    const int b = blockIdx.y % batch, l = blockIdx.y / batch;
+    if (threadIdx.x < 64) {
+      const PageDeal d = deal_pages(lens, n_valid, batch, n_q, max_ctx, n_rep, n_splits, m_tiles);
+      int32_t first = 0;   // (tokens of) partials of the requests before b
+      for (int i = 0; i < b; ++i) first += __builtin_amdgcn_readlane(d.n, i) * __builtin_amdgcn_readlane(d.tok, i);
+      if ((int)threadIdx.x == b) {
+        n_lds = d.n;
+        tok_lds = d.tok;
+        first_lds = d.dealt ? first : -1;
+      }
+    }
+    __syncthreads();
+    const int64_t first = __builtin_amdgcn_readfirstlane(first_lds), rows = (int64_t)__builtin_amdgcn_readfirstlane(tok_lds) * n_q_heads;
+    if (row >= rows) return;
+    part = row;
+    row += (int64_t)blockIdx.y * n_q * n_q_heads;
+    if (first >= 0) {
+      part += ((int64_t)l * n_splits * batch * n_q + first) * n_q_heads;
+      stride = rows;
+      n_splits = __builtin_amdgcn_readfirstlane(n_lds);
+      if (n_splits == 1) return;   // (done)
+    } else {
+      part = row;
+    }
+  }
   if (row >= rows_total) return;
-  if (n_valid || lens) {   // row = ((l * B + b) * n_q + i) * Hq + h
+  if (!kDealt && (n_valid || lens)) {   // row = ((l * B + b) * n_q + i) * Hq + h
     const int64_t ti = row / n_q_heads;
     const int i = (int)(ti % n_q);
     const int b = (int)((ti / n_q) % batch);
@@ -1369,10 +1501,10 @@ __global__ void __launch_bounds__(256) prefill_combine_kernel(const PT* __restri
 #pragma unroll
     for (int u = 0; u < kCombineBatch; ++u) {
       const int64_t s = s0 + u;
-      mls[u] = s < n_splits ? ws_ml[s * rows_total + row] : make_float2(-INFINITY, 0.f);
+      mls[u] = s < n_splits ? ws_ml[s * stride + part] : make_float2(-INFINITY, 0.f);
 #pragma unroll
       for (int i = 0; i < kPieces; ++i)
-        xs[u][i] = s < n_splits ? reinterpret_cast<const uint4*>(ws_o + (s * rows_total + row) * HD + d)[i]
+        xs[u][i] = s < n_splits ? reinterpret_cast<const uint4*>(ws_o + (s * stride + part) * HD + d)[i]
                                 : uint4{0u, 0u, 0u, 0u};
     }
 #pragma unroll
@@ -1581,18 +1713,22 @@ hipError_t launch_hd(const AttnShape& s, const PrefillArgs& a, const SplitPlan& 
     hipLaunchKernelGGL((prefill_bf16_kernel<HD, kModeSuffix, false>), grid, dim3(kThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_splits == 1) return e;
-  const dim3 cgrid((unsigned)((a.rows_total + kCombineRowsPerWG - 1) / kCombineRowsPerWG));
+  const int64_t crows = a.may_deal ? (int64_t)n_q * s.n_q_heads : a.rows_total;
+  const dim3 cgrid((unsigned)((crows + kCombineRowsPerWG - 1) / kCombineRowsPerWG), a.may_deal ? s.n_layers * s.batch : 1);
   const dim3 cblock(kCombineRowsPerWG * HD / 8);
   const bool pages = mode == kModePages || mode == kModePagesRope;
   const int32_t* nv = mode == kModeTable || pages ? a.n_valid : nullptr;
   const int32_t* lens = pages ? a.ctx_len : nullptr;
   auto combine = [&](auto* ws_o, auto batch) {
-    hipLaunchKernelGGL((prefill_combine_kernel<HD, decltype(batch)::value, std::remove_pointer_t<decltype(ws_o)>>), cgrid,
-                       cblock, 0, stream, ws_o, a.ws_ml, p.n_splits, a.rows_total, nv, lens, n_q, s.n_q_heads, s.batch, a.out);
+    auto* kernel = a.may_deal ? prefill_combine_kernel<HD, decltype(batch)::value, std::remove_pointer_t<decltype(ws_o)>, true>
+                           : prefill_combine_kernel<HD, decltype(batch)::value, std::remove_pointer_t<decltype(ws_o)>, false>;
+    hipLaunchKernelGGL(kernel, cgrid, cblock, 0, stream, ws_o, a.ws_ml, p.n_splits, a.rows_total, nv, lens, n_q, s.n_q_heads,
+                       s.batch, a.max_ctx, a.n_rep, a.m_tiles, a.out);
   };
   auto combine_as = [&](auto* ws_o) {
-    if (p.n_splits <= 4) combine(ws_o, std::integral_constant<int, 4>{});
-    else if (p.n_splits <= 8) combine(ws_o, std::integral_constant<int, 8>{});
+    const int batch = p.n_splits;
+    if (batch <= 4) combine(ws_o, std::integral_constant<int, 4>{});
+    else if (batch <= 8) combine(ws_o, std::integral_constant<int, 8>{});
     else combine(ws_o, std::integral_constant<int, 16>{});
   };
   if (p.f32_partials) combine_as(static_cast<float*>(a.ws_o));
@@ -1617,6 +1753,7 @@ hipError_t launch(const AttnShape& s, PrefillArgs a, int mode, bool interleaved,
   a.m_tiles = p.m_tiles;
   a.n_splits = p.n_splits;
   a.tiles_per_split = p.tiles_per_split;
+  a.may_deal = (mode == kModePages || mode == kModePagesRope) && suffix_dealt(p.n_splits, s.batch);
   a.n_wg = p.m_tiles * p.n_splits * s.batch * s.n_kv_heads;
   // Inline layouts: m-tiles differ in length (the first sees a prefix, the last everything), and a
   // launch ended with the last pairs' long m-tiles alone on the chip.  Short launches go m-tile by

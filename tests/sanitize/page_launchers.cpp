@@ -168,9 +168,9 @@ hipError_t launch_decode_bf16_pages(const PageAttnArgs& a) {
 }
 
 namespace {
-// A bf16 suffix call: `splits` ranges of the request's keys, whole units of `unit` each.
-template <typename F, typename G>
-hipError_t walk_suffix(const PageAttnArgs& a, int splits, int unit, F partial, G combined) {
+// A bf16 suffix call: request b's keys in splits_of(b) equal ranges, whole units of `unit` each.
+template <typename S, typename F, typename G>
+hipError_t walk_suffix(const PageAttnArgs& a, S splits_of, int unit, F partial, G combined) {
   ++emu::launches;
   const AttnShape& s = a.s;
   const int n_rep = s.n_q_heads / s.n_kv_heads;
@@ -180,19 +180,21 @@ hipError_t walk_suffix(const PageAttnArgs& a, int splits, int unit, F partial, G
         const Stream st(a, 2, l, b, g);
         if (st.n_tok == 0) continue;
         const int n_vis = st.ctx + st.n_tok;
+        const int splits = splits_of(b);
+        if (splits < 1) return hipErrorInvalidValue;
         const int64_t chunk = (int64_t)ceil_div(ceil_div(n_vis, unit), splits) * unit;
         for (int sp = 0; sp < splits; ++sp) {
           const int wc0 = (int)std::min(sp * chunk, (int64_t)n_vis), wc1 = (int)std::min(wc0 + chunk, (int64_t)n_vis);
           st.keys(wc0, wc1);
           for (int i = 0; i < st.n_tok; ++i)
-            for (int h = g * n_rep; h < (g + 1) * n_rep; ++h) partial(st.q_row(i, h), sp);
+            for (int h = g * n_rep; h < (g + 1) * n_rep; ++h) partial(l, b, i, h, st, sp);
         }
         for (int i = 0; i < st.n_tok; ++i) {
           st.store(i);
           st.turn(st.ctx + i);
           for (int h = g * n_rep; h < (g + 1) * n_rep; ++h) {
             rd(a.q, st.q_row(i, h), st.rb());
-            combined(st.q_row(i, h));
+            combined(l, b, i, h, st);
             wr(a.out, st.q_row(i, h), st.rb());
           }
         }
@@ -207,11 +209,11 @@ hipError_t launch_few_bf16_pages(const PageAttnArgs& a) {
   const int64_t rows = (int64_t)s.n_layers * s.batch * a.n_new * s.n_q_heads;
   float* ws_o = static_cast<float*>(a.workspace);
   float* ws_ml = n > 1 ? ws_o + rows * n * s.head_dim : nullptr;
-  return walk_suffix(a, n, kDecodeUnit, [&](int64_t row, int sp) {
+  return walk_suffix(a, [&](int) { return n; }, kDecodeUnit, [&](int, int, int i, int h, const Stream& st, int sp) {
     if (n == 1) return;
-    wr(ws_o, row * n + sp, (int64_t)s.head_dim * 4);
-    wr(ws_ml, row * n + sp, 8);
-  }, [](int64_t) {});
+    wr(ws_o, st.q_row(i, h) * n + sp, (int64_t)s.head_dim * 4);
+    wr(ws_ml, st.q_row(i, h) * n + sp, 8);
+  }, [](int, int, int, int, const Stream&) {});
 }
 
 hipError_t launch_prefill_bf16_pages(const PageAttnArgs& a) {
@@ -220,12 +222,52 @@ hipError_t launch_prefill_bf16_pages(const PageAttnArgs& a) {
   const int64_t rows = (int64_t)s.n_layers * s.batch * a.n_new * s.n_q_heads;
   const int64_t part = (int64_t)s.head_dim * (p.f32_partials ? 4 : 2);
   uint8_t* ws_o = static_cast<uint8_t*>(a.workspace);
-  return walk_suffix(a, p.n_splits, kPrefillKeys, [&](int64_t row, int sp) {
-    if (p.n_splits == 1) return;
-    wr(ws_o, sp * rows + row, part);
-    wr(ws_o + p.n_splits * rows * part, sp * rows + row, 8);
-  }, [&](int64_t row) {
-    for (int sp = 0; p.n_splits > 1 && sp < p.n_splits; ++sp) rd(ws_o, sp * rows + row, part);
+  std::vector<int32_t> n(s.batch, p.n_splits), first(s.batch, 0);
+  bool dealt = suffix_dealt(p.n_splits, s.batch);
+  if (dealt) {
+    const int n_rep = s.n_q_heads / s.n_kv_heads;
+    std::vector<int32_t> u(s.batch, 0), t(s.batch), m(s.batch);
+    int64_t total = 0;
+    int32_t longest = 0, c = 0;
+    for (int b = 0; b < s.batch; ++b) {
+      t[b] = page_new_tokens(a.base_len, a.n_valid, b, a.n_new);
+      m[b] = ceil_div(t[b] * n_rep, kPrefillRowsPerWG);
+      if (t[b] > 0) u[b] = ceil_div(clamp_len(a.base_len[b], a.max_base) + t[b], kPrefillKeys);
+      total += (int64_t)u[b] * m[b];
+      longest = std::max(longest, u[b]);
+    }
+    if (longest == 0) {
+      ++emu::launches;
+      return hipSuccess;
+    }
+    const RangeCandidates rc = suffix_range_candidates(total, longest, p.n_splits, s.batch * p.m_tiles);
+    for (int i = 0; i < kDecodeDealt; ++i) {
+      c = rc.at(i);
+      int64_t wgs = 0, parts = 0;
+      for (int b = 0; b < s.batch; ++b) {
+        n[b] = ceil_div(u[b], c);
+        wgs += (int64_t)n[b] * m[b];
+        parts += (int64_t)n[b] * t[b];
+      }
+      if (wgs <= (int64_t)p.n_splits * s.batch * p.m_tiles && parts <= (int64_t)p.n_splits * s.batch * a.n_new) break;
+      if (i == kDecodeDealt - 1) return hipErrorInvalidValue;   // the last candidate always fits
+    }
+    dealt = suffix_deal_pays(c, rc.top);
+    if (!dealt) n.assign(s.batch, p.n_splits);
+    for (int b = 1; b < s.batch; ++b) first[b] = first[b - 1] + n[b - 1] * t[b - 1];
+  }
+  // a row's partial of range sp
+  auto slot = [&](int l, int b, int i, int h, const Stream& st, int sp) {
+    if (!dealt) return sp * rows + st.q_row(i, h);
+    return ((int64_t)l * p.n_splits * s.batch * a.n_new + first[b] + (int64_t)sp * st.n_tok + i) * s.n_q_heads + h;
+  };
+  return walk_suffix(a, [&](int b) { return n[b]; }, kPrefillKeys,
+                     [&](int l, int b, int i, int h, const Stream& st, int sp) {
+    if (n[b] == 1) return;
+    wr(ws_o, slot(l, b, i, h, st, sp), part);
+    wr(ws_o + p.n_splits * rows * part, slot(l, b, i, h, st, sp), 8);
+  }, [&](int l, int b, int i, int h, const Stream& st) {
+    for (int sp = 0; n[b] > 1 && sp < n[b]; ++sp) rd(ws_o, slot(l, b, i, h, st, sp), part);
   });
 }
 

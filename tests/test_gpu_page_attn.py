@@ -244,6 +244,68 @@ def test_lengths_are_clamped():
     check(x)
 
 
+DEALT = {   # one or two long requests among short ones, padded tokens, requests of padding only
+    "padding": ((32, 8, 128), 40, [9001, 20, -1, 0, 700], [40, 1, 7, 40, 0], 1),
+    "row tiles": ((28, 4, 128), 100, [6000, 6000, 100, 90, 80, 70], [100, 3, 100, 100, 64, 65], 1),
+    "layers": ((8, 2, 64), 67, [4161, 30, 1000], [67, 64, 5], 2),
+    "float32 partials": ((32, 8, 128), 128, [9000] + [200] * 7, [128] * 7 + [1], 1),
+    "64 requests": ((4, 1, 128), 64, [8000, 7000] + [100] * 62, [64] * 63 + [0], 1),
+    "many ranges": ((4, 1, 64), 40, [10] * 20 + [20000] + [10] * 19, [40] * 40, 1),
+    "alone": ((16, 2, 64), 40, [-1, -1, 5000, -1], [40] * 4, 1),
+    "65 requests": ((4, 1, 128), 64, [8000] + [100] * 64, [64] * 65, 1),   # too many to deal
+}
+
+
+@pytest.mark.parametrize("name", list(DEALT))
+@pytest.mark.parametrize("rope", [False, True])
+def test_suffix_uneven_requests(name, rope):
+    """Split launches that deal their ranges by length."""
+    (hq, hkv, d), n, ctx, new, L = DEALT[name]
+    x = setup(hq, hkv, d, "bf16", 16 if rope else 64, ctx, new, n=n, L=L, slack=3)
+    assert pic.pic_prefill_workspace_bytes(x.model, x.B, x.n, x.max_ctx) > 0
+    if not rope:
+        suffix(x)
+        return check(x)
+    # against the turned rows
+    y = setup(hq, hkv, d, "bf16", 16, ctx, new, n=n, L=L, slack=3)
+    r = rope_table(x)
+    pos = torch.tensor([[max(c, 0) + i for i in range(n)] for c in ctx], dtype=torch.int32, device=DEV)
+    for t, h in ((y.q, hq), (y.k, hkv)):
+        for l in range(L):
+            pic.pic_rerotate_keys(y.model, t[l], t[l], y.B * n, h, pos, *r)
+    suffix(x, rope=r)
+    suffix(y)
+    assert (x.out == y.out).all()
+    assert (x.pk.view(torch.int16) == y.pk.view(torch.int16)).all()
+
+
+def test_dealt_ranges_follow_the_lengths_in_a_graph():
+    """Lengths that change between the replays of a captured call: other ranges, the bits of an eager call."""
+    x = setup(32, 8, 128, "bf16", 64, [8000, 7900, 6000, 5000], [40] * 4, n=40)
+    ws = torch.full((pic.pic_prefill_workspace_bytes(x.model, x.B, x.n, x.max_ctx),), 0xFF, dtype=torch.uint8, device=DEV)
+    x.pk.nan_to_num_(0.5)   # (rows past a request's end are read once its length has grown)
+    x.pv.nan_to_num_(0.5)
+    suffix(x, ws=ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        suffix(x, ws=ws)
+    for ctx, new in (([8000, 10, 10, 10], [40] * 4), ([8000] * 4, [40] * 4), ([-1, 7000, 3, -1], [40, 40, 2, 40]),
+                     ([10, 10, 10, 8000], [1, 40, 0, 40]), ([-1] * 4, [40] * 4), ([5, 5, 5, 5], [3] * 4), ([8000, 10, 10, 10], [40] * 4)):
+        ctx = [min(c, x.ctx[b]) for b, c in enumerate(ctx)]   # (as far as its pages reach)
+        x.len.copy_(torch.tensor(ctx, dtype=torch.int32))
+        x.n_valid.copy_(torch.tensor(new, dtype=torch.int32))
+        x.out.fill_(SENTINEL)
+        suffix(x, ws=ws)
+        want = x.out.clone()
+        for _ in range(2):
+            x.out.fill_(SENTINEL)
+            ws.fill_(0xFF)
+            g.replay()
+            torch.cuda.synchronize()
+            assert (x.out.view(torch.int16) == want.view(torch.int16)).all(), (ctx, new)
+
+
 @pytest.mark.parametrize("kind", ["decode", "few", "suffix"])
 def test_contexts_far_below_the_bound(kind):
     """A call's bound on the lengths far above them, as a captured step has it: every request's own keys split."""
