@@ -490,11 +490,12 @@ pic_status pic_page_copy(const pic_model* model, const pic_pages* pages, void* p
 
 /* ---- 5c. suffix prefill over pages ----
    pic_suffix_prefill_attn on a paged cache: stores k_suf / v_suf of token i < n_valid[b] of request
-   b at slot ctx_len[b] + i and computes its attention over slots [0, ctx_len[b] + i].  Up to 32 query rows
-   (tokens x query heads) per kv head may run on a kernel of their own, which keeps probabilities to 16
-   bits.  max_ctx costs little where contexts are shorter: a launch split over the keys splits every
-   request's own, long requests into more ranges than short ones where that ends the launch earlier (of
-   up to 64 requests), so the last bits of an output may depend on the lengths of the other requests.
+   b at slot ctx_len[b] + i and computes its attention over slots [0, ctx_len[b] + i].  Up to 32 query
+   rows (tokens x query heads) per kv head may run on a kernel of their own, which keeps probabilities to
+   16 bits; others round them to 8.  max_ctx costs little where contexts are shorter: a launch split over
+   the keys splits every request's own, long requests into more ranges than short ones where that ends
+   the launch earlier (of up to 64 requests), so the last bits of an output may depend on the lengths of
+   the other requests.
      page_table [device, batch x table_cap]
      ctx_len    [device, batch]   clamped to max_ctx; a negative one marks a request that is only
                                   padding: nothing of it is read, stored or computed
@@ -503,7 +504,8 @@ pic_status pic_page_copy(const pic_model* model, const pic_pages* pages, void* p
      max_ctx + n_suffix <= table_cap * page_tokens and <= 2^30 (PIC_ERR_CAPACITY)
      (q, k_suf, v_suf, out, scale and the workspace as for pic_suffix_prefill_attn; bf16 pages:
      n_pages * page_tokens and n_suffix * Hkv below 2^24)
-   pic_page_suffix_attn_rope: q and k_suf unrotated, as for pic_suffix_prefill_attn_rope.  bf16 only. */
+   pic_page_suffix_attn_rope: q and k_suf unrotated, as for pic_suffix_prefill_attn_rope.  bf16 only.  Turned
+   queries keep 16 bits, or 8 where more than 32 rows at head_dim 128 go to the prefill kernel. */
 pic_status pic_page_suffix_attn(const pic_model* model, const pic_pages* pages, const void* q,
                                 const void* k_suf, const void* v_suf, void* pages_k, void* pages_v,
                                 const int32_t* page_table, int32_t batch, const int32_t* ctx_len,
@@ -526,7 +528,8 @@ pic_status pic_page_suffix_attn_rope(const pic_model* model, const pic_pages* pa
                                   nothing of that request is read or stored, its out rows are left untouched
      max_base_len + step + 1 <= table_cap * page_tokens and <= 2^30 (PIC_ERR_CAPACITY)
      (the other arguments and the workspace as for pic_decode_attn)
-   pic_page_decode_attn_rope: q and k_new unrotated, as for pic_decode_attn_rope.  bf16 only. */
+   pic_page_decode_attn_rope: q and k_new unrotated, as for pic_decode_attn_rope; turned queries keep 16
+   bits.  bf16 only. */
 pic_status pic_page_decode_attn(const pic_model* model, const pic_pages* pages, const void* q,
                                 const void* k_new, const void* v_new, void* pages_k, void* pages_v,
                                 const int32_t* page_table, int32_t batch, const int32_t* base_len,

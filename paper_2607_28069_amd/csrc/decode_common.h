@@ -130,12 +130,27 @@ __device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
   return u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
                pack_bf16x2(x[6], x[7])};
 }
+// x in two bfloat16 terms
+__device__ __forceinline__ void pack8_terms(const float (&x)[8], u32x4& hi, u32x4& lo) {
+  float h[8], r[8];
+  hi = pack8(x);
+  unpack8(hi, h);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = x[e] - h[e];
+  lo = pack8(r);
+}
 // The head dims 32 ks + 8 g4 .. + 8 (ks < HD/32) a lane holds of one row (the A / B operand
 // layout below), turned by row `trow` of the table: rotate-half pairs are chunks ks and
 // ks + HD/64 (frequencies 32 ks + 8 g4 + j), interleaved pairs sit inside a chunk (16 ks + 4 g4 + m).
+// With `lo`, what the rounding to bfloat16 leaves.
 template <int HD, bool kInterleaved>
-__device__ __forceinline__ void rot_operand(u32x4 (&c)[Dims<HD>::kSteps], const float2* trow, int g4) {
+__device__ __forceinline__ void rot_operand(u32x4 (&c)[Dims<HD>::kSteps], const float2* trow, int g4,
+                                            u32x4 (*lo)[Dims<HD>::kSteps] = nullptr) {
   constexpr int KS = Dims<HD>::kSteps;
+  auto put = [&](int ks, const float (&x)[8]) {
+    if (lo) pack8_terms(x, c[ks], (*lo)[ks]);
+    else c[ks] = pack8(x);
+  };
   if constexpr (!kInterleaved) {
 #pragma unroll
     for (int ks = 0; ks < KS / 2; ++ks) {
@@ -147,8 +162,8 @@ __device__ __forceinline__ void rot_operand(u32x4 (&c)[Dims<HD>::kSteps], const 
         const float2 cs = trow[32 * ks + 8 * g4 + j];
         rot_pair(x[j], y[j], cs.x, cs.y);
       }
-      c[ks] = pack8(x);
-      c[ks + KS / 2] = pack8(y);
+      put(ks, x);
+      put(ks + KS / 2, y);
     }
   } else {
 #pragma unroll
@@ -160,7 +175,7 @@ __device__ __forceinline__ void rot_operand(u32x4 (&c)[Dims<HD>::kSteps], const 
         const float2 cs = trow[16 * ks + 4 * g4 + m];
         rot_pair(x[2 * m], x[2 * m + 1], cs.x, cs.y);
       }
-      c[ks] = pack8(x);
+      put(ks, x);
     }
   }
 }

@@ -15,7 +15,8 @@
 //    call allows 33K 24.1 -> 15.4, 16 of 5K where it allows 20K 81.9 -> 59.3; 16 of 8K to 16K 140 -> 146).
 //  * Probabilities enter the product with V as two bfloat16 terms, the rounded value and what the
 //    rounding left (2^-17 relative to the value then).  The matrix cores have the time: 0.5 to 2 %, and
-//    the output's error against 64 bits falls from 0.0023 to that of its own rounding, 0.0017.
+//    the output's error against 64 bits falls from 0.0023 to that of its own rounding, 0.0017.  The rope
+//    variant keeps two terms of its turned queries as well (0.3 to 1.5 %, 0.0024 -> 0.0017).
 //  * The new token is stored after the key loop, with a table entry that nothing waited for; the
 //    queries are turned (rope variant) with the first tile's rows on their way.
 //  * Requests with a negative length are padding of the batch: their workgroups leave at once, and
@@ -160,8 +161,9 @@ page_decode_kernel(PageDecodeArgs a) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qv[ks] = ok ? qp[4 * ks + g4] : u32x4{0, 0, 0, 0};
   }
+  u32x4 q_lo[KS];   // rope variant: what rounding the turned query to bfloat16 left
   auto take_q = [&]() {
-    if constexpr (kRope) rot_operand<HD, kInterleaved>(qv, trow, g4);
+    if constexpr (kRope) rot_operand<HD, kInterleaved>(qv, trow, g4, &q_lo);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qop[ks] = as_bf16x8(qv[ks]);
   };
@@ -236,8 +238,11 @@ page_decode_kernel(PageDecodeArgs a) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int mb = 0; mb < 2; ++mb)
+      for (int mb = 0; mb < 2; ++mb) {
         sacc[mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kcur[mb][ks]), qop[ks], sacc[mb], 0, 0, 0);
+        if constexpr (kRope)
+          sacc[mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kcur[mb][ks]), as_bf16x8(q_lo[ks]), sacc[mb], 0, 0, 0);
+      }
     float mx = -INFINITY;
 #pragma unroll
     for (int mb = 0; mb < 2; ++mb)

@@ -7,7 +7,8 @@
 // whatever the loads do.  Here, as in decode, every wave takes all the rows and an eighth of the workgroup's keys,
 // and the waves' results merge by log-sum-exp: the launch is bound by the bytes of K and V again.
 //  * Row r = token r / n_rep, head r % n_rep, along N of v_mfma_f32_16x16x32_bf16 in one or two blocks of
-//    16; tiles, page numbers, K and V moves and the two-term probabilities as in page_decode.hip.
+//    16; tiles, page numbers, K and V moves, and probabilities and turned queries in two terms as in
+//    page_decode.hip.
 //  * A row sees the keys up to its own token: the last tiles are masked per row, and a row that a wave's
 //    keys all lie past has no reference maximum there and adds nothing.
 //  * A probability of 0 times a value that is not finite is no 0: new tokens' values that are not finite
@@ -52,6 +53,11 @@ page_few_kernel(PageFewArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t v_lds0[kFewWaves * kVTileBytes];
   __shared__ __attribute__((aligned(16))) uint8_t v_lds1[kFewWaves * kVTileBytes];
   __shared__ float ml_lds[kFewWaves * ROWS * 2];
+  // rope variant: the turned queries in two bfloat16 terms, the same in every wave; at head_dim 128 those of two
+  // blocks of rows have no room in registers (16 requests of 10K x 8 tokens 165 us; the second terms in LDS 132,
+  // both 126)
+  constexpr bool kQueryLds = kRope && HD == 128 && NB == 2;
+  __shared__ __attribute__((aligned(16))) u32x4 q_lds[kQueryLds ? 2 * NB * KS * 64 : 1];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -119,12 +125,19 @@ page_few_kernel(PageFewArgs a) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qv[nb][ks] = ok ? qp[4 * ks + g4] : u32x4{0, 0, 0, 0};
   }
+  u32x4 q_lo[NB][KS];
   auto take_q = [&]() {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      if constexpr (kRope) rot_operand<HD, kInterleaved>(qv[nb], trow(qpos[nb]), g4);
+      if constexpr (kRope) rot_operand<HD, kInterleaved>(qv[nb], trow(qpos[nb]), g4, &q_lo[nb]);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) qop[nb][ks] = as_bf16x8(qv[nb][ks]);
+      for (int ks = 0; ks < KS; ++ks) {
+        qop[nb][ks] = as_bf16x8(qv[nb][ks]);
+        if constexpr (kQueryLds) {   // (all waves write the same)
+          q_lds[(nb * KS + ks) * 64 + lane] = qv[nb][ks];
+          q_lds[((NB + nb) * KS + ks) * 64 + lane] = q_lo[nb][ks];
+        }
+      }
     }
   };
 
@@ -206,6 +219,8 @@ page_few_kernel(PageFewArgs a) {
         }
       }
     }
+    int q_at = lane;
+    if constexpr (kQueryLds) asm volatile("" : "+v"(q_at));   // (read for each tile, not kept in registers)
     f32x4_t sacc[NB][2];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) sacc[nb][0] = sacc[nb][1] = f32x4_t{};
@@ -214,8 +229,14 @@ page_few_kernel(PageFewArgs a) {
 #pragma unroll
       for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          sacc[nb][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kcur[mb][ks]), qop[nb][ks], sacc[nb][mb], 0, 0, 0);
+        for (int nb = 0; nb < NB; ++nb) {
+          const bf16x8_t hi = kQueryLds ? as_bf16x8(q_lds[(nb * KS + ks) * 64 + q_at]) : qop[nb][ks];
+          sacc[nb][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kcur[mb][ks]), hi, sacc[nb][mb], 0, 0, 0);
+          if constexpr (kRope) {
+            const u32x4 lo = kQueryLds ? q_lds[((NB + nb) * KS + ks) * 64 + q_at] : q_lo[nb][ks];
+            sacc[nb][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kcur[mb][ks]), as_bf16x8(lo), sacc[nb][mb], 0, 0, 0);
+          }
+        }
     // probabilities in bfloat16, and what that rounding left
     bf16x8_t pop_h[NB], pop_l[NB];
 #pragma unroll

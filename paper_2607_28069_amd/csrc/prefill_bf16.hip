@@ -102,6 +102,9 @@ __device__ __forceinline__ void dma16_other(rsrc_t r, uint32_t voff, void* lds) 
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x8_t __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ bf16x8_t as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8_t, v); }
 
@@ -172,9 +175,10 @@ struct PrefillArgs {
   int32_t n_wg;             // m_tiles * n_splits * batch * n_kv_heads
   int32_t tail_bgs;         // table mode: pairs per XCD dispatched m-tile by m-tile (0: none)
   int64_t rows_total;       // L * batch * n_suffix * Hq (query rows of one split's partials)
-  void* ws_o;               // [n_splits][rows_total][D] each split's normalised output, bf16 or
-  int32_t f32_partials;     // float32
-  float2* ws_ml;            // [n_splits][rows_total] (reference max, row sum)
+  void* ws_o;               // [n_splits][rows_total][D] each split's normalised output, bf16 (pages modes:
+  int32_t f32_partials;     // half, scaled) or float32
+  float2* ws_ml;            // [n_splits][rows_total] (reference max, row sum); half: (log2 of the sum with its
+                            // reference, scale)
   float scale_log2;
   PageMap map;              // pages modes: cache_k / cache_v are [L][Hkv][stream_rows][D]
   int32_t stream_rows;
@@ -590,6 +594,14 @@ prefill_bf16_kernel(PrefillArgs a) {
 
   // ---- Q^T operand: lane (n, hh) holds q[row n][16 ks + 8 hh .. +8) for ks = 0 .. D / 16 - 1
   bf16x8_t qop[kKS];
+  // pages mode with RoPE at head_dim 64: what rounding the turned queries to bfloat16 left.  Its products cost
+  // 10 to 13 % (5 requests of 2K to 4K keys x 1 to 67 tokens 31.0 -> 34.0 us, 16 of 4K x 200 171 -> 193) and take
+  // the turn's rounding out of the scores (2-norm error against 64 bits of the 5 0.0026 -> 0.0022).  At 128
+  // there are no registers for it, and launches are bound by the power of the matrix cores, which it would use
+  // half as much again: there queries are rounded, as in the rope mode.  Probabilities in two terms as well
+  // would cost another 18 % at 64 (34.0 -> 40.1): they are rounded.
+  constexpr bool kTwoTerms = kMode == kModePagesRope && HD == 64;
+  bf16x8_t q_lo[kTwoTerms ? kKS : 1];
   {
     const u32x4* qp = reinterpret_cast<const u32x4*>(a.q + (row_ok ? row_at(r, tok) : 0) * kHD);
 #pragma unroll
@@ -598,6 +610,17 @@ prefill_bf16_kernel(PrefillArgs a) {
   // rope mode: queries turned to their positions (called once the first tiles' loads are in
   // flight, so the table reads overlap them)
   auto rope_q = [&]() {
+    auto put = [&](int ks, const float (&x)[8]) {
+      const u32x4 hi = pack8(x);
+      qop[ks] = as_bf16x8(hi);
+      if constexpr (kTwoTerms) {
+        float h[8], rest[8];
+        unpack8(hi, h);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rest[e] = x[e] - h[e];
+        q_lo[ks] = as_bf16x8(pack8(rest));
+      }
+    };
     const float2* trow = a.table + (int64_t)l * a.table_stride + (int64_t)min(qpos, a.max_abs_delta) * (kHD / 2);
     if constexpr (!kInterleaved) {
       // pairs (d, d + D / 2): operand steps ks and ks + D / 32, frequencies 16 ks + 8 hh .. + 7
@@ -607,8 +630,8 @@ prefill_bf16_kernel(PrefillArgs a) {
         unpack8(__builtin_bit_cast(u32x4, qop[ks]), x1);
         unpack8(__builtin_bit_cast(u32x4, qop[ks + kKS / 2]), x2);
         rot_chunks<false>(x1, x2, trow, 16 * ks + 8 * hh);
-        qop[ks] = as_bf16x8(pack8(x1));
-        qop[ks + kKS / 2] = as_bf16x8(pack8(x2));
+        put(ks, x1);
+        put(ks + kKS / 2, x2);
       }
     } else {
       // pairs (2i, 2i + 1) inside each chunk: dims 16 ks + 8 hh + 2m, frequency 8 ks + 4 hh + m
@@ -621,7 +644,7 @@ prefill_bf16_kernel(PrefillArgs a) {
           const float2 cs = trow[8 * ks + 4 * hh + m];
           rot_pair(x[2 * m], x[2 * m + 1], cs.x, cs.y);
         }
-        qop[ks] = as_bf16x8(pack8(x));
+        put(ks, x);
       }
     }
   };
@@ -980,6 +1003,7 @@ prefill_bf16_kernel(PrefillArgs a) {
       for (int kb2 = 0; kb2 < 2; ++kb2) {
         const u32x4 kv = *reinterpret_cast<const u32x4*>(kt + k_rd[ks] + 32 * kb2 * kRowBytes);
         s[kb2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kv), qop[ks], s[kb2], 0, 0, 0);
+        if constexpr (kTwoTerms) s[kb2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kv), q_lo[ks], s[kb2], 0, 0, 0);
       }
   };
 
@@ -1251,6 +1275,8 @@ prefill_bf16_kernel(PrefillArgs a) {
           const int pj = j / kJPer, ks = (kKS / 4) * s4 + (pj >> 1), kb = pj & 1;
           if (kb == 0) snext[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kq[ks][0]), qop[ks], ks == 0 ? f32x16_t{} : snext[0], 0, 0, 0);
           else snext[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kq[ks][1]), qop[ks], ks == 0 ? f32x16_t{} : snext[1], 0, 0, 0);
+          if constexpr (kTwoTerms)
+            snext[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kq[ks][kb]), q_lo[ks], snext[kb], 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);
           if (ks + 2 < kKS) kq[ks + 2][kb] = kread(ks + 2, kb);
         }
@@ -1349,9 +1375,28 @@ prefill_bf16_kernel(PrefillArgs a) {
   int lane_e = lane;
   asm volatile("" : "+v"(lane_e));
   const int n_e = lane_e & 31, hh_e = lane_e >> 5;
+  // Pages modes: a share in 16 bits is kept in half precision (11 bits, not 8), scaled by the power of two above
+  // the row's largest finite value, and m and l as one number: what a split launch adds to the error against
+  // 64 bits goes (5 requests of 2K to 4K keys, head_dim 64: 0.0022 -> 0.0018), for 0.7 us.
+  int share_exp = 0;
+  if constexpr (kPages) {
+    if (n_ranges > 1 && !a.f32_partials) {
+      float share_max = 0.f;
+#pragma unroll
+      for (int db = 0; db < kDB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float x = fabsf(oacc[db][e]);
+          share_max = fmaxf(share_max, x < INFINITY ? x : 0.f);
+        }
+      share_exp = min(max(__builtin_amdgcn_frexp_expf(pair_max(share_max) / l_tot), -100), 120);
+    }
+  }
   if (n_ranges > 1 && hh_e == 0 && row_ok) {
     const int r2 = row0_wg + wave * kRowsPerWave + n_e;
-    a.ws_ml[part0() + row_at(r2, div_rep(r2))] = make_float2(m_run, l_tot);
+    a.ws_ml[part0() + row_at(r2, div_rep(r2))] =
+        !kPages || a.f32_partials ? make_float2(m_run, l_tot)
+                                  : make_float2(m_run == -INFINITY ? m_run : m_run + log2f(l_tot), ldexpf(1.f, share_exp));
   }
   if (!wave_rows) return;
   // Normalised: the output in bf16, or one split's share of it in bf16 or float32 (with its
@@ -1416,13 +1461,20 @@ prefill_bf16_kernel(PrefillArgs a) {
       wave_sync();
     }
   } else {
+    const bool half = kPages && n_ranges > 1;
+    const float to_one = half ? ldexpf(1.f, -share_exp) : 1.f;
 #pragma unroll
     for (int db = 0; db < kDB; ++db)
 #pragma unroll
       for (int qd = 0; qd < 4; ++qd) {
         uint2 v;
-        v.x = pack_bf16x2(oacc[db][4 * qd] * inv, oacc[db][4 * qd + 1] * inv);
-        v.y = pack_bf16x2(oacc[db][4 * qd + 2] * inv, oacc[db][4 * qd + 3] * inv);
+        if (half) {
+          const f32x4_t x = f32x4_t{oacc[db][4 * qd], oacc[db][4 * qd + 1], oacc[db][4 * qd + 2], oacc[db][4 * qd + 3]} * inv * to_one;
+          v = __builtin_bit_cast(uint2, __builtin_convertvector(x, f16x4_t));
+        } else {
+          v.x = pack_bf16x2(oacc[db][4 * qd] * inv, oacc[db][4 * qd + 1] * inv);
+          v.y = pack_bf16x2(oacc[db][4 * qd + 2] * inv, oacc[db][4 * qd + 3] * inv);
+        }
         *reinterpret_cast<uint2*>(stage + chunk_at(n_e, 4 * db + qd) + 8 * hh_e) = v;
       }
     wave_sync();
@@ -1432,8 +1484,9 @@ prefill_bf16_kernel(PrefillArgs a) {
 }
 
 // Merge the key-range splits of each query row by log-sum-exp.  Split s left its output
-// normalised by its own row sum l_s (PT: bf16 or float32) with its reference max m_s: the row is
-// sum_s w_s O_s / sum_s w_s with w_s = 2^(m_s - M) l_s, M any common reference.  grid (rows_total / 16),
+// normalised by its own row sum l_s (PT: bf16, half or float32) with its reference max m_s: the row is
+// sum_s w_s O_s / sum_s w_s with w_s = 2^(m_s - M) l_s, M any common reference.  PT half (pages modes): with
+// m_s + log2(l_s) in the place of m_s, and the factor of the row's values in that of l_s.  grid (rows_total / 16),
 // 2 D threads: D / 8 lanes per row, 8 head dims per lane; every split's loads are issued without a branch
 // between them (a split that saw no key of the row, reference max -inf, is dropped by a
 // select: its sums are not finite).  With n_valid (table and pages modes), rows of tokens past
@@ -1453,6 +1506,7 @@ __global__ void __launch_bounds__(256) prefill_combine_kernel(const PT* __restri
                                                               int32_t m_tiles, bf16_t* __restrict__ out) {
   constexpr int kLanes = HD / 8;   // lanes per row
   constexpr int kPieces = sizeof(PT) / 2;   // 16-byte pieces of a lane's 8 head dims
+  constexpr bool kHalf = __is_same(PT, _Float16);
   int64_t row = (int64_t)blockIdx.x * kCombineRowsPerWG + threadIdx.x / kLanes;
   int64_t part = row, stride = rows_total;   // a row's partials: the first one's place, from one to the next
   if constexpr (kDealt) {
@@ -1513,11 +1567,15 @@ __global__ void __launch_bounds__(256) prefill_combine_kernel(const PT* __restri
     const bool seen = ml.x != -INFINITY;
     const float m_new = seen ? fmaxf(M, ml.x) : M;
     const float keep = seen ? __builtin_amdgcn_exp2f(M - m_new) : 1.f;   // 0 while M is -inf
-    const float w = seen ? __builtin_amdgcn_exp2f(ml.x - m_new) * ml.y : 0.f;
+    const float e = seen ? __builtin_amdgcn_exp2f(ml.x - m_new) : 0.f, w = seen ? e * ml.y : 0.f;
     M = m_new;
-    den = den * keep + w;
+    den = den * keep + (kHalf ? e : w);
     float x[8];
-    if constexpr (kPieces == 1) {
+    if constexpr (kHalf) {
+      const f32x8_t y = __builtin_convertvector(__builtin_bit_cast(f16x8_t, xs[u][0]), f32x8_t);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = y[i];
+    } else if constexpr (kPieces == 1) {
       unpack8(u32x4{xs[u][0].x, xs[u][0].y, xs[u][0].z, xs[u][0].w}, x);
     } else {
 #pragma unroll
@@ -1732,6 +1790,7 @@ hipError_t launch_hd(const AttnShape& s, const PrefillArgs& a, const SplitPlan& 
     else combine(ws_o, std::integral_constant<int, 16>{});
   };
   if (p.f32_partials) combine_as(static_cast<float*>(a.ws_o));
+  else if (pages) combine_as(static_cast<_Float16*>(a.ws_o));
   else combine_as(static_cast<bf16_t*>(a.ws_o));
   return hipGetLastError();
 }

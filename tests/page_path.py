@@ -48,6 +48,7 @@ def setup(hq, hkv, d, dtype, P, ctx, new, n=None, L=1, spare=3, seed=0, slack=0,
     x.n_valid = torch.tensor(list(new), dtype=torch.int32, device=DEV)
     x.out = torch.full((L, B, n, hq, d), SENTINEL, dtype=dt, device=DEV)
     x.model = pic.Model.of(L, hq, hkv, d, dtype, 5e5, pairing)
+    x.pairing = pairing
     return x
 
 
@@ -61,6 +62,26 @@ def rope_table(x):
     t = torch.empty(pic.pic_rope_table_bytes(x.model, mad) // 4, dtype=torch.float32, device=DEV)
     pic.pic_rope_table_init(x.model, mad, t)
     return t, mad
+
+
+def turn(x, rope):
+    """The queries and new keys of `x` turned to their slots by rows of the table: keys as pic_rerotate_keys rounds
+    them, in x.k and x.K, queries in 64 bits in x.q.  Returns the queries as pic_rerotate_keys rounds them."""
+    table, mad = rope
+    pos = torch.tensor([[max(c, 0) + i for i in range(x.n)] for c in x.ctx], dtype=torch.int32, device=DEV)
+    interleaved = x.pairing == "interleaved"
+    cs = table.view(-1, x.d // 2, 2)[pos.long()].double()[:, :, None]   # [B, n, 1, D / 2, 2], every layer's
+    q = x.q.double()
+    a, b = (q[..., ::2], q[..., 1::2]) if interleaved else (q[..., : x.d // 2], q[..., x.d // 2:])
+    a, b = a * cs[..., 0] - b * cs[..., 1], b * cs[..., 0] + a * cs[..., 1]
+    rounded = x.q.clone()
+    for t, h in ((rounded, x.hq), (x.k, x.hkv)):
+        pic.pic_rerotate_keys(x.model, t, t, x.L * x.B * x.n, h, pos.repeat(x.L, 1, 1).contiguous(), table, mad)
+    x.q = torch.stack([a, b], -1).flatten(-2) if interleaved else torch.cat([a, b], -1)
+    for i in range(x.B):
+        m = x.new[i] if x.ctx[i] >= 0 else 0
+        x.K[i] = torch.cat([x.K[i][:, :, : x.K[i].shape[2] - m], x.k[:, i, :m].transpose(1, 2)], 2)
+    return rounded
 
 
 def decode(x, step=0, n_splits=0, ws="query", rope=None, scale=0.0, **kw):
@@ -117,13 +138,16 @@ def reference(x, scale=0.0):
     return out, mag, score
 
 
-def check(x, scale=0.0, decoded=False):
+def check(x, scale=0.0, decoded=False, turned=False):
     """Outputs within the rounding of their arithmetic (u = 2^-24 the float32 half step, T the keys):
       float32   scores: D products summed, off by D u sum|q k| scale; probabilities off by that
                 relative to themselves, in numerator and denominator; sums of T terms by T u each
       bf16      besides: the output rounded (2^-8); in a prefill also each probability (2^-8), which the
-                numerator and the denominator see, and a split's share (2^-8); in a decode the probabilities
-                are two bfloat16 terms (2^-16)
+                numerator and the denominator see, and a split's share (2^-11 in half precision, whose
+                smallest step is 2^-24 of the row's largest value); in a decode the probabilities are two
+                bfloat16 terms (2^-16)
+      turned    (x.q in 64 bits) queries turned in float32 and then two bfloat16 terms: 2^-16 of each, and of
+                the float32 turn 2^-22 of its pair, so scores off by 2^-16 sum|q k| scale
     rows of padding untouched, page rows holding exactly the tokens, everything else as it was."""
     ref, mag, score = reference(x, scale)
     got = x.out.double()
@@ -131,7 +155,10 @@ def check(x, scale=0.0, decoded=False):
     u = 2.0 ** -24
     tol = (2 * x.d * u * score + 2 * (T + 16) * u) * mag + 1e-30
     if x.dtype == "bf16":
-        tol = tol + (2 * 2.0 ** -16 if decoded else 3 * 2.0 ** -8) * mag + 2.0 ** -8 * ref.abs()
+        tol = tol + (2 * 2.0 ** -16 if decoded else 2 * 2.0 ** -8 + 2.0 ** -11) * mag + 2.0 ** -8 * ref.abs()
+        tol = tol + (0 if decoded else 2.0 ** -25 * mag.sum(-1, keepdim=True))
+    if turned:
+        tol = tol + 2 * 2.0 ** -16 * (1 + 2.0 ** -4) * score * mag
     pad = torch.ones((x.B, x.n), dtype=torch.bool, device=DEV)
     for b in range(x.B):
         pad[b, : x.new[b] if x.ctx[b] >= 0 else 0] = False
@@ -143,10 +170,11 @@ def check(x, scale=0.0, decoded=False):
     assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} outputs off, worst {float((err / tol)[:, live].max()):.2f} of the bound"
     if live.any():
         rel = float(err[:, live].norm() / ref[:, live].norm())
-        # float32 sums wander by the root of their terms; each of the one or three bf16 roundings is 2^-8 / sqrt(3)
-        # in the 2-norm, independent of one another
+        # float32 sums wander by the root of their terms; each of the one or two bf16 roundings is 2^-8 / sqrt(3)
+        # in the 2-norm, independent of one another (a share's 2^-11 in what two leave of 2^-8)
         most = 2 * u * (math.sqrt(x.d) * float(score.max()) + math.sqrt(T) + 8)
         most += 2.0 ** -8 / (math.sqrt(3) if decoded else 1) if x.dtype == "bf16" else 0
+        most += 2 * 2.0 ** -16 * float(score.max()) if turned else 0
         assert rel <= most, (rel, most)
     check_pages(x)
 

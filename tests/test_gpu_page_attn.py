@@ -7,9 +7,26 @@ import pytest
 import torch
 
 import paper_2607_28069_amd as pic
-from page_path import DEV, SENTINEL, check, contiguous, decode, reference, rope_table, rows, setup, suffix
+from page_path import DEV, SENTINEL, check, check_pages, contiguous, decode, reference, rope_table, rows, setup, suffix, turn
 
 pytestmark = pytest.mark.gpu
+
+def check_rope(x, call, rounds):
+    """Queries and keys turned by the call.  rounds: the call rounds turned queries to bfloat16, and gives bit for
+    bit what turning them with pic_rerotate_keys first gives; else it keeps 16 bits of them (None: either)."""
+    r = rope_table(x)
+    call(x, rope=r)
+    out, rounded = x.out.clone(), turn(x, r)
+    check_pages(x)   # (keys: bit for bit in either case)
+    exact, x.q = x.q, rounded
+    x.out.fill_(SENTINEL)
+    call(x)
+    same = bool((x.out == out).all())
+    assert rounds is None or same == rounds
+    if not same:
+        x.q, x.out = exact, out
+    check(x, turned=not same, decoded=call is decode)
+
 
 HEADS = [(4, 2, 64), (32, 8, 128), (28, 4, 128), (5, 1, 64), (3, 3, 128), (40, 1, 128)]
 
@@ -87,20 +104,8 @@ def test_suffix_few_rows(hq, hkv, d, n, batch):
     new = [max(n - i % (n + 1), 0) if batch != "lone" else n for i in range(len(ctx))]
     for P, rope in ((16, False), (64, True)):
         x = setup(hq, hkv, d, "bf16", P, ctx, new, n=n, slack=3)
-        if rope:   # against the turned rows
-            y = setup(hq, hkv, d, "bf16", P, ctx, new, n=n, slack=3)
-            r = rope_table(x)
-            pos = torch.tensor([[max(c, 0) + i for i in range(n)] for c in ctx], dtype=torch.int32, device=DEV)
-            for t, h in ((y.q, hq), (y.k, hkv)):
-                pic.pic_rerotate_keys(y.model, t, t, y.B * n, h, pos, *r)
-            suffix(x, rope=r)
-            suffix(y)
-            assert (x.out == y.out).all()
-            assert (x.pk.view(torch.int16) == y.pk.view(torch.int16)).all()
-            for b in range(y.B):
-                m = new[b] if ctx[b] >= 0 else 0
-                y.K[b] = torch.cat([y.K[b][:, :, : y.K[b].shape[2] - m], y.k[:, b, :m].transpose(1, 2)], 2)
-            check(y)
+        if rope:
+            check_rope(x, suffix, False if d == 64 else None)   # (at 128 some sizes go to the prefill kernel)
         else:
             suffix(x)
             check(x)
@@ -111,21 +116,27 @@ def test_suffix_few_rows(hq, hkv, d, n, batch):
     (8, 2, 64, 200, [4000]), (32, 8, 128, 128, [190] * 12), (8, 2, 128, 9, [6000, 6000]), (32, 8, 128, 256, [1000, 64, 3, 700])])
 @pytest.mark.parametrize("rope", [False, True])
 def test_suffix_bits_of_the_contiguous_call(hq, hkv, d, n, ctx, rope):
-    """The prefill kernel over pages is the contiguous one: same bits where both split the keys alike (contexts
-    of one length, or no split)."""
+    """The prefill kernel over pages is the contiguous one: same bits where turned queries are rounded alike and
+    the keys are not split, or split alike with float32 shares.  With shares in 16 bits the contiguous call's are
+    off by 2^-8 where those over pages are by 2^-11, and each output by its own 2^-8: root mean squares
+    2^-8 / sqrt(3), three of them."""
+    if rope and d == 64:
+        return
     for P in (16, 64, 512):
         x = setup(hq, hkv, d, "bf16", P, ctx, [n] * len(ctx), L=2)
         ck, cv, cap = contiguous(x)
         r = rope_table(x) if rope else None
         suffix(x, rope=r, n_valid=None if P == 64 else "given")
-        ws = torch.empty(max(pic.pic_prefill_workspace_bytes(x.model, x.B, n, x.max_ctx), 16), dtype=torch.uint8, device=DEV)
+        size = pic.pic_prefill_workspace_bytes(x.model, x.B, n, x.max_ctx)
+        ws = torch.empty(max(size, 16), dtype=torch.uint8, device=DEV)
         out = torch.empty_like(x.out)
         args = (x.model, x.q, x.k, x.v, ck, cv, x.B, cap, x.len, x.max_ctx, n)
         if rope:
             pic.pic_suffix_prefill_attn_rope(*args, *r, out, ws)
         else:
             pic.pic_suffix_prefill_attn(*args, out, ws)
-        assert (out == x.out).all()
+        if not (out == x.out).all():
+            assert size > 0 and float((out.double() - x.out.double()).norm() / out.double().norm()) <= 2.0 ** -8 * 1.05
         for b in range(x.B):
             r0 = rows(x, b, 0, ctx[b] + n)
             for p, c in ((x.pk, ck), (x.pv, cv)):
@@ -164,29 +175,15 @@ def test_suffix_long_split_over_keys():
         check(x)
 
 
-@pytest.mark.parametrize("kind", ["decode", "suffix"])
+@pytest.mark.parametrize("kind", ["decode", "few", "suffix"])
 @pytest.mark.parametrize("pairing", ["half", "interleaved"])
 @pytest.mark.parametrize("d", [64, 128])
-def test_rope_is_turning_first(kind, pairing, d):
-    """Unrotated rows in: bit for bit what turning them with pic_rerotate_keys first gives."""
-    ctx, new = [0, 17, 640, -1, 2000], [1] * 5 if kind == "decode" else [21, 3, 21, 21, 0]
-    n = 1 if kind == "decode" else 21
+def test_rope_turns_first(kind, pairing, d):
+    """Unrotated rows in."""
+    n = {"decode": 1, "few": 4, "suffix": 21}[kind]
+    ctx, new = [0, 17, 640, -1, 2000], [1] * 5 if kind == "decode" else [n, 3, n, n, 0]
     x = setup(8, 2, d, "bf16", 32, ctx, new, n=n, pairing=pairing, L=2)
-    y = setup(8, 2, d, "bf16", 32, ctx, new, n=n, pairing=pairing, L=2)
-    rope = rope_table(x)
-    call = decode if kind == "decode" else suffix
-    call(x, rope=rope)
-    pos = torch.tensor([[max(c, 0) + i for i in range(n)] for c in ctx], dtype=torch.int32, device=DEV)
-    for t, h in ((y.q, y.hq), (y.k, y.hkv)):
-        pic.pic_rerotate_keys(y.model, t, t, y.L * y.B * n, h, pos.repeat(y.L, 1, 1).contiguous(), *rope)
-    call(y)
-    assert (x.out == y.out).all()
-    for a, b in ((x.pk, y.pk), (x.pv, y.pv)):
-        assert (a.view(torch.int16) == b.view(torch.int16)).all()
-    for b in range(y.B):   # and those outputs are right
-        m = y.new[b] if ctx[b] >= 0 else 0
-        y.K[b] = torch.cat([y.K[b][:, :, : y.K[b].shape[2] - m], y.k[:, b, :m].transpose(1, 2)], 2)
-    check(y, decoded=kind == "decode")
+    check_rope(x, decode if kind == "decode" else suffix, kind == "suffix" and d == 128)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -263,20 +260,10 @@ def test_suffix_uneven_requests(name, rope):
     (hq, hkv, d), n, ctx, new, L = DEALT[name]
     x = setup(hq, hkv, d, "bf16", 16 if rope else 64, ctx, new, n=n, L=L, slack=3)
     assert pic.pic_prefill_workspace_bytes(x.model, x.B, x.n, x.max_ctx) > 0
-    if not rope:
-        suffix(x)
-        return check(x)
-    # against the turned rows
-    y = setup(hq, hkv, d, "bf16", 16, ctx, new, n=n, L=L, slack=3)
-    r = rope_table(x)
-    pos = torch.tensor([[max(c, 0) + i for i in range(n)] for c in ctx], dtype=torch.int32, device=DEV)
-    for t, h in ((y.q, hq), (y.k, hkv)):
-        for l in range(L):
-            pic.pic_rerotate_keys(y.model, t[l], t[l], y.B * n, h, pos, *r)
-    suffix(x, rope=r)
-    suffix(y)
-    assert (x.out == y.out).all()
-    assert (x.pk.view(torch.int16) == y.pk.view(torch.int16)).all()
+    if rope:
+        return check_rope(x, suffix, d == 128)
+    suffix(x)
+    check(x)
 
 
 def test_dealt_ranges_follow_the_lengths_in_a_graph():
