@@ -1377,7 +1377,8 @@ prefill_bf16_kernel(PrefillArgs a) {
   const int n_e = lane_e & 31, hh_e = lane_e >> 5;
   // Pages modes: a share in 16 bits is kept in half precision (11 bits, not 8), scaled by the power of two above
   // the row's largest finite value, and m and l as one number: what a split launch adds to the error against
-  // 64 bits goes (5 requests of 2K to 4K keys, head_dim 64: 0.0022 -> 0.0018), for 0.7 us.
+  // 64 bits goes (5 requests of 2K to 4K keys, head_dim 64: 0.0022 -> 0.0018), for 0.7 us.  (Values 2^-17 of their row's largest, and smaller ones,
+  // keep fewer bits than in bfloat16: the last is 2^-24 of the largest.)
   int share_exp = 0;
   if constexpr (kPages) {
     if (n_ranges > 1 && !a.f32_partials) {
@@ -1389,7 +1390,7 @@ prefill_bf16_kernel(PrefillArgs a) {
           const float x = fabsf(oacc[db][e]);
           share_max = fmaxf(share_max, x < INFINITY ? x : 0.f);
         }
-      share_exp = min(max(__builtin_amdgcn_frexp_expf(pair_max(share_max) / l_tot), -100), 120);
+      share_exp = min(max(__builtin_amdgcn_frexp_expf(pair_max(share_max) / l_tot), -126), 120);
     }
   }
   if (n_ranges > 1 && hh_e == 0 && row_ok) {

@@ -266,6 +266,22 @@ def test_suffix_uneven_requests(name, rope):
     check(x)
 
 
+@pytest.mark.parametrize("value_scale", [1e-33, 1e-7, 1e5, 1e33])
+@pytest.mark.parametrize("d", [64, 128])
+def test_split_shares_of_any_magnitude(value_scale, d):
+    """Shares of a split launch in half precision: values far past its range, and rows of one huge value (whose
+    other values are as good as that one's last bits)."""
+    x = setup(8, 2, d, "bf16", 16, [5000, 300], [40, 40], slack=3, value_scale=value_scale)
+    assert pic.pic_prefill_workspace_bytes(x.model, x.B, x.n, x.max_ctx) > 0
+    suffix(x)
+    check(x)
+    x = setup(8, 2, d, "bf16", 16, [5000, 300], [40, 40], slack=3)
+    x.pv[:, :, rows(x, 0, 17, 18), 3] *= value_scale   # (one head dim of one key)
+    x.V[0][:, :, 17, 3] *= value_scale
+    suffix(x)
+    check(x)
+
+
 def test_dealt_ranges_follow_the_lengths_in_a_graph():
     """Lengths that change between the replays of a captured call: other ranges, the bits of an eager call."""
     x = setup(32, 8, 128, "bf16", 64, [8000, 7900, 6000, 5000], [40] * 4, n=40)
