@@ -522,7 +522,8 @@ pic_status pic_page_suffix_attn_rope(const pic_model* model, const pic_pages* pa
    pic_decode_attn on a paged cache: stores the new token at slot p = base_len[b] + step and attends
    over slots [0, p]; split over the context and joined alike.  On bf16 pages probabilities keep 16 bits
    where pic_decode_attn rounds them to 8, so outputs carry little more than their own rounding, and the
-   ranges of a split launch are those of each request's own keys.
+   ranges of a split launch are those of each request's own keys.  A NaN in a query or a visible key makes the outputs
+   it enters NaN, here and in 5c, however the keys are split.
      page_table [device, batch x table_cap]
      base_len   [device, batch]   clamped to max_base_len; a negative one marks padding of the batch:
                                   nothing of that request is read or stored, its out rows are left untouched

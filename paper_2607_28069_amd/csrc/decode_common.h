@@ -28,6 +28,10 @@ struct Dims {
 static_assert(kDecodeUnit == kWaves * kTile, "a unit is one tile per wave");
 static_assert(kWaves == kDecodeWaves && kMinWaveKeys == kDecodeMinWaveKeys, "host split planner tiling");
 constexpr int kNonTemporal = 2;                    // cache-policy bits of a streaming load
+// Decode over pages: the reference maximum of a row before its first key.  Finite, so that a row without keys, or
+// whose scores are all -inf, has probabilities, and in a merge a weight, of 0 times 0, and one whose scores
+// are NaN (which a maximum passes over) brings its NaN sums into the merge.
+constexpr float kNoMax = -3.402823466e38f;
 
 #define LDS_AS __attribute__((address_space(3)))
 #define GLOBAL_AS __attribute__((address_space(1)))
@@ -185,7 +189,7 @@ __device__ __forceinline__ void rot_operand(u32x4 (&c)[Dims<HD>::kSteps], const 
 // hold 4 head dims each of one range, 1024 / HD ranges side by side, and every range's loads are
 // issued before any is used; the range groups then merge in LDS.  (One wave walking the ranges
 // took 4.9 us for 8 or 32 of them: a memory round trip per 8, once for the maxima and once for
-// the sums.)  A range that saw no key (maximum -inf) adds nothing.
+// the sums.)  A range that saw no key (maximum -inf; over pages kNoMax and sums of 0) adds nothing.
 // (pages, heads > 0: `heads` query rows for each of n_new tokens per request, n_q_heads counting them all)
 struct FewTokens {
   const int32_t* n_valid = nullptr;

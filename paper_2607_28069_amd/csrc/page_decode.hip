@@ -218,7 +218,7 @@ page_decode_kernel(PageDecodeArgs a) {
   f32x4_t oacc[DB];
 #pragma unroll
   for (int i = 0; i < DB; ++i) oacc[i] = f32x4_t{};
-  float m_run = -INFINITY, l_part = 0.f;
+  float m_run = kNoMax, l_part = 0.f;
   const bf16x2_t ones = __builtin_bit_cast(bf16x2_t, 0x3F803F80u);
 
   // One tile at k0, resident in kcur and buffer P; the next one's loads are issued first, and have
@@ -354,15 +354,13 @@ page_decode_kernel(PageDecodeArgs a) {
   // thread -> (query n = tid / KC, head dims 8 (tid % KC) .. +8)
   const int mn = tid / KC, md = 8 * (tid & (KC - 1));
   if (mn < n_here) {
-    float M = -INFINITY;
+    float M = kNoMax;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) M = fmaxf(M, ml_lds[(w * 16 + mn) * 2]);
     float den = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float mw = ml_lds[(w * 16 + mn) * 2];
-      if (mw == -INFINITY) continue;   // an empty wave range
-      const float wt = __builtin_amdgcn_exp2f(mw - M);
+      const float wt = __builtin_amdgcn_exp2f(ml_lds[(w * 16 + mn) * 2] - M);
       den += wt * ml_lds[(w * 16 + mn) * 2 + 1];
       const f32x4_t x0 = *o_lds(w, mn, md / 4), x1 = *o_lds(w, mn, md / 4 + 1);
 #pragma unroll

@@ -10,7 +10,7 @@
 //    16; tiles, page numbers, K and V moves, and probabilities and turned queries in two terms as in
 //    page_decode.hip.
 //  * A row sees the keys up to its own token: the last tiles are masked per row, and a row that a wave's
-//    keys all lie past has no reference maximum there and adds nothing.
+//    keys all lie past keeps its first reference maximum there and adds nothing.
 //  * A probability of 0 times a value that is not finite is no 0: new tokens' values that are not finite
 //    are cleared in LDS, and added at the end to the rows that see them.
 //  * The new tokens' rows come from k_new / v_new (keys turned on load in the rope variant) and are stored
@@ -185,7 +185,7 @@ page_few_kernel(PageFewArgs a) {
   float m_run[NB], l_part[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    m_run[nb] = -INFINITY;
+    m_run[nb] = kNoMax;
     l_part[nb] = 0.f;
 #pragma unroll
     for (int i = 0; i < DB; ++i) oacc[nb][i] = f32x4_t{};
@@ -255,18 +255,17 @@ page_few_kernel(PageFewArgs a) {
       const float m_tile = mx * a.scale_log2;
       if (__any(m_tile > m_run[nb] + 8.f)) {   // lazy reference max: p <= 2^8, which nothing below minds
         const float m_new = fmaxf(m_run[nb], m_tile);
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[nb] - m_new);
+        const float alpha = __builtin_amdgcn_exp2f(m_run[nb] - m_new);
         m_run[nb] = m_new;
         l_part[nb] *= alpha;
 #pragma unroll
         for (int db = 0; db < DB; ++db) oacc[nb][db] *= alpha;
       }
-      const float m_use = m_run[nb] == -INFINITY ? 0.f : m_run[nb];   // (a row that has seen no key yet)
       uint32_t ph[4], pl[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(sacc[nb][j >> 1][2 * (j & 1)], a.scale_log2, -m_use));
-        const float p1 = __builtin_amdgcn_exp2f(fmaf(sacc[nb][j >> 1][2 * (j & 1) + 1], a.scale_log2, -m_use));
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(sacc[nb][j >> 1][2 * (j & 1)], a.scale_log2, -m_run[nb]));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(sacc[nb][j >> 1][2 * (j & 1) + 1], a.scale_log2, -m_run[nb]));
         ph[j] = pack_bf16x2(p0, p1);
         pl[j] = pack_bf16x2(p0 - __uint_as_float(ph[j] << 16), p1 - __uint_as_float(ph[j] & 0xFFFF0000u));
       }
@@ -382,15 +381,13 @@ page_few_kernel(PageFewArgs a) {
   __syncthreads();
   for (int item = tid; item < M * KC; item += kFewThreads) {   // (row, 8 head dims)
     const int r = item / KC, md = 8 * (item & (KC - 1));
-    float m_all = -INFINITY;
+    float m_all = kNoMax;
 #pragma unroll
     for (int w = 0; w < kFewWaves; ++w) m_all = fmaxf(m_all, ml_lds[(w * ROWS + r) * 2]);
     float den = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kFewWaves; ++w) {
-      const float mw = ml_lds[(w * ROWS + r) * 2];
-      if (mw == -INFINITY) continue;   // no key of this row
-      const float wt = __builtin_amdgcn_exp2f(mw - m_all);
+      const float wt = __builtin_amdgcn_exp2f(ml_lds[(w * ROWS + r) * 2] - m_all);
       den += wt * ml_lds[(w * ROWS + r) * 2 + 1];
       const f32x4_t x0 = *o_lds(w, r, md / 4), x1 = *o_lds(w, r, md / 4 + 1);
 #pragma unroll

@@ -1395,9 +1395,11 @@ prefill_bf16_kernel(PrefillArgs a) {
   }
   if (n_ranges > 1 && hh_e == 0 && row_ok) {
     const int r2 = row0_wg + wave * kRowsPerWave + n_e;
+    // pages: a maximum passes over NaN, so a row whose scores here are all NaN has none either; its sums count
+    const float m_row = kPages && m_run == -INFINITY && qpos >= t0 * kKeys ? NAN : m_run;
     a.ws_ml[part0() + row_at(r2, div_rep(r2))] =
-        !kPages || a.f32_partials ? make_float2(m_run, l_tot)
-                                  : make_float2(m_run == -INFINITY ? m_run : m_run + log2f(l_tot), ldexpf(1.f, share_exp));
+        !kPages || a.f32_partials ? make_float2(m_row, l_tot)
+                                  : make_float2(m_row == -INFINITY ? m_row : m_row + log2f(l_tot), ldexpf(1.f, share_exp));
   }
   if (!wave_rows) return;
   // Normalised: the output in bf16, or one split's share of it in bf16 or float32 (with its
