@@ -496,6 +496,10 @@ pic_status pic_page_copy(const pic_model* model, const pic_pages* pages, void* p
    the keys splits every request's own, long requests into more ranges than short ones where that ends
    the launch earlier (of up to 64 requests), so the last bits of an output may depend on the lengths of
    the other requests.
+   What is not finite (here and in 5d): a NaN in a query or a visible key makes the outputs it enters NaN, however the
+   keys are split; the visible values that are not finite are, in their head dim, summed up in place of the
+   average; what no token sees changes nothing.  On bf16 pages averages are finite for values up to 2^120 over the
+   number of keys: larger ones may overflow on the way.
      page_table [device, batch x table_cap]
      ctx_len    [device, batch]   clamped to max_ctx; a negative one marks a request that is only
                                   padding: nothing of it is read, stored or computed
@@ -522,8 +526,7 @@ pic_status pic_page_suffix_attn_rope(const pic_model* model, const pic_pages* pa
    pic_decode_attn on a paged cache: stores the new token at slot p = base_len[b] + step and attends
    over slots [0, p]; split over the context and joined alike.  On bf16 pages probabilities keep 16 bits
    where pic_decode_attn rounds them to 8, so outputs carry little more than their own rounding, and the
-   ranges of a split launch are those of each request's own keys.  A NaN in a query or a visible key makes the outputs
-   it enters NaN, here and in 5c, however the keys are split.
+   ranges of a split launch are those of each request's own keys.
      page_table [device, batch x table_cap]
      base_len   [device, batch]   clamped to max_base_len; a negative one marks padding of the batch:
                                   nothing of that request is read or stored, its out rows are left untouched

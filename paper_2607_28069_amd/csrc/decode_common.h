@@ -4,6 +4,7 @@
 
 #include <algorithm>
 
+#include "odd_values.h"
 #include "pic_bounds.h"
 #include "pic_internal.h"
 
@@ -250,6 +251,12 @@ __global__ void __launch_bounds__(256) decode_combine_kernel(const float* __rest
       o = o * keep + w * x[u];
     }
   }
+  if constexpr (kPages) {
+    const int64_t slot0 = layer0 + (int64_t)place.first * n_q_heads + (int64_t)h * place.n;
+    float y[4] = {o[0], o[1], o[2], o[3]};
+    odd_partials(y, (place.n - grp + kGroups - 1) / kGroups, [&](int i, int e) { return ws_o[(slot0 + grp + i * kGroups) * HD + d + e]; });
+    o = f32x4_t{y[0], y[1], y[2], y[3]};
+  }
   *reinterpret_cast<f32x4_t*>(o_s + grp * HD + d) = o;
   if (d == 0) {
     m_s[grp] = M;
@@ -260,18 +267,19 @@ __global__ void __launch_bounds__(256) decode_combine_kernel(const float* __rest
   float m_all = -INFINITY;
 #pragma unroll
   for (int g = 0; g < kGroups; ++g) m_all = fmaxf(m_all, m_s[g]);
-  float l_all = 0.f, o0 = 0.f, o1 = 0.f;
+  float l_all = 0.f, y[2] = {0.f, 0.f};
 #pragma unroll
   for (int g = 0; g < kGroups; ++g) {
     if (m_s[g] == -INFINITY) continue;
     const float w = __builtin_amdgcn_exp2f(m_s[g] - m_all);
     l_all += w * l_s[g];
-    o0 += w * o_s[g * HD + 2 * threadIdx.x];
-    o1 += w * o_s[g * HD + 2 * threadIdx.x + 1];
+    y[0] += w * o_s[g * HD + 2 * threadIdx.x];
+    y[1] += w * o_s[g * HD + 2 * threadIdx.x + 1];
   }
+  if constexpr (kPages) odd_partials(y, kGroups, [&](int g, int e) { return o_s[g * HD + 2 * threadIdx.x + e]; });
   const float inv = 1.f / l_all;
   const int64_t row = ((int64_t)l * batch + b) * n_q_heads + h;
-  reinterpret_cast<uint32_t*>(out + row * HD)[threadIdx.x] = pack_bf16x2(o0 * inv, o1 * inv);
+  reinterpret_cast<uint32_t*>(out + row * HD)[threadIdx.x] = pack_bf16x2(y[0] * inv, y[1] * inv);
 }
 
 

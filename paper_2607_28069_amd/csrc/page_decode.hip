@@ -17,6 +17,8 @@
 //    rounding left (2^-17 relative to the value then).  The matrix cores have the time: 0.5 to 2 %, and
 //    the output's error against 64 bits falls from 0.0023 to that of its own rounding, 0.0017.  The rope
 //    variant keeps two terms of its turned queries as well (0.3 to 1.5 %, 0.0024 -> 0.0017).
+//  * A value that is not finite reaches the outputs in its head dim, whatever its probability (odd_values); the
+//    merge sees it by 8 additions a thread, which do not show in any time.
 //  * The new token is stored after the key loop, with a table entry that nothing waited for; the
 //    queries are turned (rope variant) with the first tile's rows on their way.
 //  * Requests with a negative length are padding of the batch: their workgroups leave at once, and
@@ -254,7 +256,7 @@ page_decode_kernel(PageDecodeArgs a) {
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     const float m_tile = mx * a.scale_log2;
-    if (__any(m_tile > m_run + 8.f)) {   // lazy reference max: p <= 2^8, which nothing below minds
+    if (__any(m_tile > m_run + 8.f)) {   // lazy reference max: p <= 2^8 (so values up to 2^120 over the number of keys)
       const float m_new = fmaxf(m_run, m_tile);
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
@@ -353,11 +355,10 @@ page_decode_kernel(PageDecodeArgs a) {
   __syncthreads();
   // thread -> (query n = tid / KC, head dims 8 (tid % KC) .. +8)
   const int mn = tid / KC, md = 8 * (tid & (KC - 1));
+  float M = kNoMax, den = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (mn < n_here) {
-    float M = kNoMax;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) M = fmaxf(M, ml_lds[(w * 16 + mn) * 2]);
-    float den = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const float wt = __builtin_amdgcn_exp2f(ml_lds[(w * 16 + mn) * 2] - M);
@@ -369,6 +370,16 @@ page_decode_kernel(PageDecodeArgs a) {
         o[4 + e] += wt * x1[e];
       }
     }
+  }
+  // values that are not finite (where the scores are: else the outputs are NaN anyway)
+  if (__any(any_odd(o) && fabsf(den) < INFINITY)) {
+    float v[8] = {};
+    odd_values<KC>([&](int key) { return key == p ? Vn : Vg + page_row(a.map, b, key) * HD; }, wc0, wc1, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (!(fabsf(v[e]) < INFINITY)) o[e] = v[e];
+  }
+  if (mn < n_here) {
     const int64_t row = ((int64_t)l * a.batch + b) * a.n_q_heads + g * n_rep + rep0 + mn;
     if (place.n == 1) {
       const float inv = 1.f / den;

@@ -12,7 +12,8 @@
 //  * A row sees the keys up to its own token: the last tiles are masked per row, and a row that a wave's
 //    keys all lie past keeps its first reference maximum there and adds nothing.
 //  * A probability of 0 times a value that is not finite is no 0: new tokens' values that are not finite
-//    are cleared in LDS, and added at the end to the rows that see them.
+//    are cleared in LDS, so that rows that do not see them stay as they are.  Those, and cached ones, reach the rows
+//    that see them when the waves merge (odd_values).
 //  * The new tokens' rows come from k_new / v_new (keys turned on load in the rope variant) and are stored
 //    into their pages by the workgroup whose range holds them.
 #include <type_traits>
@@ -53,6 +54,7 @@ page_few_kernel(PageFewArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t v_lds0[kFewWaves * kVTileBytes];
   __shared__ __attribute__((aligned(16))) uint8_t v_lds1[kFewWaves * kVTileBytes];
   __shared__ float ml_lds[kFewWaves * ROWS * 2];
+  __shared__ bool odd_lds[kFewWaves];   // a value of the new tokens in a wave's keys was not finite
   // rope variant: the turned queries in two bfloat16 terms, the same in every wave; at head_dim 128 those of two
   // blocks of rows have no room in registers (16 requests of 10K x 8 tokens 165 us; the second terms in LDS 132,
   // both 126)
@@ -253,7 +255,7 @@ page_few_kernel(PageFewArgs a) {
       mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
       const float m_tile = mx * a.scale_log2;
-      if (__any(m_tile > m_run[nb] + 8.f)) {   // lazy reference max: p <= 2^8, which nothing below minds
+      if (__any(m_tile > m_run[nb] + 8.f)) {   // lazy reference max: p <= 2^8 (so values up to 2^120 over the number of keys)
         const float m_new = fmaxf(m_run[nb], m_tile);
         const float alpha = __builtin_amdgcn_exp2f(m_run[nb] - m_new);
         m_run[nb] = m_new;
@@ -303,20 +305,6 @@ page_few_kernel(PageFewArgs a) {
     }
   }
 
-  if (__any(odd)) {   // those values, to the rows that see them
-    for (int key = max(c0, ctx); key < c1; ++key)
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-        if (key <= qpos[nb])
-#pragma unroll
-          for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float v = bf16_to_f32(Vn[(key - ctx) * new_stride + 16 * db + 4 * g4 + e]);
-              if (!(fabsf(v) < INFINITY)) oacc[nb][db][e] += v;
-            }
-  }
-
   // The new tokens of this range into their pages (nobody reads those rows from the pages in this launch).
   for (int i = st_i; i < st1; i += kFewThreads / (2 * KC)) {
     const int slot = ctx + i;
@@ -361,6 +349,7 @@ page_few_kernel(PageFewArgs a) {
     l_tot[nb] = l_part[nb] + __shfl_xor(l_part[nb], 16, 64);
     l_tot[nb] += __shfl_xor(l_tot[nb], 32, 64);
   }
+  const bool odd_wave = __any(odd);
   __syncthreads();
   // (16-byte chunk c of row r at c ^ (r & 15): the 16 rows of a store would meet in one bank otherwise)
   auto o_lds = [&](int w, int r, int c) {
@@ -378,13 +367,19 @@ page_few_kernel(PageFewArgs a) {
       ml_lds[(wave * ROWS + r) * 2 + 1] = l_tot[nb];
     }
   }
+  if (lane == 0) odd_lds[wave] = odd_wave;
   __syncthreads();
-  for (int item = tid; item < M * KC; item += kFewThreads) {   // (row, 8 head dims)
-    const int r = item / KC, md = 8 * (item & (KC - 1));
-    float m_all = kNoMax;
+  // thread -> (row r, head dims md .. + 8)
+  static_assert(ROWS * KC <= kFewThreads, "a thread per 8 outputs");
+  const int r = tid / KC, md = 8 * (tid & (KC - 1));
+  float m_all = kNoMax, den = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  bool odd_new = false;
+  if (r < M) {
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) m_all = fmaxf(m_all, ml_lds[(w * ROWS + r) * 2]);
-    float den = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < kFewWaves; ++w) {
+      m_all = fmaxf(m_all, ml_lds[(w * ROWS + r) * 2]);
+      odd_new |= odd_lds[w];
+    }
 #pragma unroll
     for (int w = 0; w < kFewWaves; ++w) {
       const float wt = __builtin_amdgcn_exp2f(ml_lds[(w * ROWS + r) * 2] - m_all);
@@ -396,6 +391,18 @@ page_few_kernel(PageFewArgs a) {
         o[4 + e] += wt * x1[e];
       }
     }
+  }
+  // values that are not finite (where the scores are: else the outputs are NaN anyway): cached ones, which every row
+  // sees, and the new tokens', up to the row's own
+  if (__any((odd_new || any_odd(o)) && fabsf(den) < INFINITY)) {
+    float v[8] = {};
+    odd_values<KC>([&](int key) { return Vg + page_row(a.map, b, key) * HD; }, wc0, min(wc1, ctx), v);
+    for (int key = max(wc0, ctx); key < wc1 && key <= ctx + r / n_rep; ++key) add_odd(Vn + (key - ctx) * new_stride + md, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (!(fabsf(v[e]) < INFINITY)) o[e] = v[e];
+  }
+  if (r < M) {
     const int64_t row = row_of(r);
     if (a.n_splits == 1) {
       const float inv = 1.f / den;

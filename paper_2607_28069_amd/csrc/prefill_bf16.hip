@@ -51,6 +51,7 @@
 #include <climits>
 #include <type_traits>
 
+#include "odd_values.h"
 #include "pic_bounds.h"
 #include "pic_internal.h"
 
@@ -920,7 +921,7 @@ prefill_bf16_kernel(PrefillArgs a) {
   auto wait_loads = [&]() { __builtin_amdgcn_s_waitcnt(0x0F70); };   // vmcnt(0)
   // Pages modes: a probability of 0 times a value that is not finite is no 0.  New tokens' values that are
   // not finite are cleared in LDS, by the lane that moved them, before any wave reads the tile, and added
-  // at the end to the rows that see them.
+  // at the end to the rows that see them.  (Cached ones: odd_values, at the end.)
   auto clear_values = [&](uint8_t* vt, int t) {   // global tile t, landed in vt
     if ((t + 1) * kKeys <= ctx) return;
 #pragma unroll
@@ -1352,8 +1353,45 @@ prefill_bf16_kernel(PrefillArgs a) {
 
   // ---- lane holds head dims 32 db + 8 qd + 4 hh + (0..3) of its row
   flush_pending();   // the last tile's last slice
+  // (lane number as the epilogue sees it: opaque, so that what follows from it is worked out here
+  // and not held in registers through the key loop)
+  int lane_e = lane;
+  asm volatile("" : "+v"(lane_e));
+  const int n_e = lane_e & 31, hh_e = lane_e >> 5;
+  // this wave's eighth of the tile buffers, which every wave is done with
+  uint8_t* const stage = (wave & 4 ? (wave & 2 ? v_lds1 : v_lds0) : (wave & 2 ? k_lds1 : k_lds0)) + (wave & 1) * (kTileBytes / 2);
+  // (the lanes of the wave read what others wrote: the compiler must keep the two apart)
+  auto wave_sync = []() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  const float l_tot = pair_sum(l_part);
   if constexpr (kPages) {
-    if (odd_lds && row_ok) {
+    // cached values that are not finite, which every row sees (where the scores are finite: else outputs are NaN)
+    float size[kDB];   // (sums of their own, for what they cost)
+#pragma unroll
+    for (int db = 0; db < kDB; ++db) {
+      size[db] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) size[db] += fabsf(oacc[db][e]);
+    }
+    if (__any(any_odd(size) && fabsf(l_tot) < INFINITY)) {
+      float v[8] = {}, *odd_row = reinterpret_cast<float*>(stage);
+      odd_values<kChunks>([&](int key) { return Vg + page_row(a.map, b, key) * kHD; }, t0 * kKeys, min((t0 + n_tiles) * kKeys, ctx), v);
+      if (lane_e < kChunks)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) odd_row[8 * lane_e + e] = v[e];
+      wave_sync();
+#pragma unroll
+      for (int db = 0; db < kDB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float x = odd_row[32 * db + 8 * (e >> 2) + 4 * hh_e + (e & 3)];
+          if (!(fabsf(x) < INFINITY)) oacc[db][e] = x;
+        }
+      wave_sync();
+    }
+    if (odd_lds && row_ok) {   // the new tokens', to the rows that see them
       for (int key = max(t0 * kKeys, ctx); key < min((t0 + n_tiles) * kKeys, qpos + 1); ++key)
 #pragma unroll
         for (int db = 0; db < kDB; ++db)
@@ -1368,13 +1406,7 @@ prefill_bf16_kernel(PrefillArgs a) {
     part = part_lds;
     n_ranges = __builtin_amdgcn_readfirstlane(ranges_lds);
   }
-  const float l_tot = pair_sum(l_part);
   const bool wave_rows = __any(row_ok);
-  // (lane number as the epilogue sees it: opaque, so that what follows from it is worked out here
-  // and not held in registers through the key loop)
-  int lane_e = lane;
-  asm volatile("" : "+v"(lane_e));
-  const int n_e = lane_e & 31, hh_e = lane_e >> 5;
   // Pages modes: a share in 16 bits is kept in half precision (11 bits, not 8), scaled by the power of two above
   // the row's largest finite value, and m and l as one number: what a split launch adds to the error against
   // 64 bits goes (5 requests of 2K to 4K keys, head_dim 64: 0.0022 -> 0.0018), for 0.7 us.  (Values 2^-17 of their row's largest, and smaller ones,
@@ -1426,13 +1458,7 @@ prefill_bf16_kernel(PrefillArgs a) {
       }
     return;
   }
-  uint8_t* const stage = (wave & 4 ? (wave & 2 ? v_lds1 : v_lds0) : (wave & 2 ? k_lds1 : k_lds0)) + (wave & 1) * (kTileBytes / 2);
   auto chunk_at = [&](int row, int c) { return row * kRowBytes + ((c ^ k_swz<HD>(row)) << 4); };
-  // (the lanes of the wave read what others wrote: the compiler must keep the two apart)
-  auto wave_sync = []() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  };
   // rows of kRowBytes bytes from the stage to base + row * stride + off (row: of out, or of a split)
   auto flush_rows = [&](uint8_t* base, int64_t stride, int off) {
     const int rows_here = M - (row0_wg + wave * kRowsPerWave);
@@ -1592,6 +1618,12 @@ __global__ void __launch_bounds__(256) prefill_combine_kernel(const PT* __restri
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = o[e] * keep + (seen ? w * x[e] : 0.f);
   }
+  }
+  if constexpr (kHalf || kPieces == 2) {   // pages modes
+    if (lens)
+      odd_partials(o, n_splits, [&](int64_t s, int e) {   // (shares of ranges that saw no key are not finite either)
+        return ws_ml[s * stride + part].x == -INFINITY ? 0.f : (float)ws_o[(s * stride + part) * HD + d + e];
+      });
   }
   const float inv = 1.f / den;
   uint4 v;
