@@ -372,6 +372,23 @@ __global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t
       den += wt * lw;
       acc += wt * *reinterpret_cast<const f32x4*>(o_lds + (w * ROWS + rr) * LROW + d);
     }
+    // pages: a probability or weight may be 0 in 32 bits where the softmax's is not; values that are not finite then
+    // count without (where the scores are finite: else the outputs are NaN anyway)
+    if (kPages && !(fabsf(acc[0]) + fabsf(acc[1]) + fabsf(acc[2]) + fabsf(acc[3]) < INFINITY) && fabsf(den) < INFINITY) {
+      f32x4 odd = {};
+      const int end = (int)pos_of(tok);
+#pragma unroll 4
+      for (int key = 0; key <= end; ++key) {
+        const float* row = key < fresh ? Vg + page_row(pg.map, b, key) * HD : a.v_new + new0 + (int64_t)(key - fresh) * new_stride;
+        const f32x4 v = *reinterpret_cast<const f32x4*>(row + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!(fabsf(v[e]) < INFINITY)) odd[e] += v[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (!(fabsf(odd[e]) < INFINITY)) acc[e] = odd[e];
+    }
     *reinterpret_cast<f32x4*>(a.out + ((lb * n_q + tok) * Hq + g * n_rep + (r - tok * n_rep)) * HD + d) = acc / den;
   }
 }

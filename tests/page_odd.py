@@ -29,7 +29,8 @@ def same_but(x, want, slack=None):
     assert torch.equal(torch.isnan(x.out), nan)
     if slack is None:
         fin = torch.zeros_like(fin)
-    assert torch.equal(x.out[~nan & ~fin].view(torch.int16), want[~nan & ~fin].view(torch.int16))
+    bits = torch.int32 if x.out.dtype == torch.float32 else torch.int16
+    assert torch.equal(x.out[~nan & ~fin].view(bits), want[~nan & ~fin].view(bits))
     err = (x.out[fin].double() - want[fin].double()).abs()
     assert (err <= (slack(want.double())[fin] if slack else 0)).all()
 
