@@ -92,9 +92,10 @@ pic::AttnShape shape_of(const pic_model* m, int32_t batch, int32_t cache_cap, fl
   return s;
 }
 
-// The workspace of a prefill of n_suffix tokens after max_ctx: what the query call says.  A launch
-// that fills half the GPU can do without and runs whole then; a workspace that is not aligned
-// counts as not brought there (it is not needed), and is refused where it is needed.
+// The workspace of a prefill of n_suffix tokens after max_ctx: what the query call says, and no more of
+// it is used, whatever is brought (calls whose query is 0 may share a buffer).  A launch that fills half the GPU
+// can do without and runs whole then; a workspace that is not aligned counts as not brought there (it is not
+// needed), and is refused where it is needed.
 pic_status check_prefill_workspace(const pic_model* m, int32_t batch, int32_t n_suffix, int32_t max_ctx,
                                    const void* workspace, size_t* ws_bytes) {
   if (m->dtype != PIC_BF16) return PIC_OK;   // (float32 attention takes none)
@@ -102,10 +103,12 @@ pic_status check_prefill_workspace(const pic_model* m, int32_t batch, int32_t n_
   if (workspace == nullptr) *ws_bytes = 0;
   if (pic::prefill_bf16_may_run_whole(s, n_suffix)) {
     if (!aligned16(workspace)) *ws_bytes = 0;
+    if (*ws_bytes > 0) *ws_bytes = std::min(*ws_bytes, pic::prefill_bf16_workspace(s, n_suffix, max_ctx));
     return PIC_OK;
   }
   const size_t need = pic::prefill_bf16_workspace(s, n_suffix, max_ctx);
   if (*ws_bytes < need) return fail(PIC_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, *ws_bytes);
+  *ws_bytes = need;
   return need > 0 ? check_ptr(workspace, "workspace") : PIC_OK;
 }
 
