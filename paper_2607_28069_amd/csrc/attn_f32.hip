@@ -101,22 +101,22 @@ __global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t
   const int n_tok = kPages ? page_new_tokens(a.pos.base, pg.n_valid, b, n_q) : n_q;
   if (kPages && n_tok == 0) return;   // padding of the batch
   auto pos_of = [&](int tok) -> int64_t { return kPages && tok >= n_tok ? -1 : a.pos(b, tok); };
-  int32_t win = 0, w_cur = 0, w_next = 0;   // entries [win, win + 64) of the page table, and the 64 after them
+  PageWindow win = {0};
+  int32_t w_cur = 0, w_next = 0;   // entries [win, win + 64) of the page table, and the 64 after them
   auto entry = [&](int32_t i) { return pg.map.table[(int64_t)b * pg.map.cap + clamp_entry(i, pg.map)]; };
   if constexpr (kPages) {
-    win = (wave * kTile) >> pg.map.shift;
-    w_cur = entry(win + lane);
-    w_next = entry(win + 64 + lane);
+    win.at = (wave * kTile) >> pg.map.shift;
+    w_cur = entry(win.at + lane);
+    w_next = entry(win.at + 64 + lane);
   }
   // pages: the row of the stream where tile t starts (t uniform, never less than the one asked for before)
   auto tile_row = [&](int t) -> int64_t {
     const int32_t e = (t * kTile) >> pg.map.shift;
-    if (e >= win + 64) {
-      win += 64;
+    if (win.moves(e, 64)) {
       w_cur = w_next;
-      w_next = entry(win + 64 + lane);
+      w_next = entry(win.at + 64 + lane);
     }
-    const int32_t page = clamp_page(__builtin_amdgcn_readlane(w_cur, e - win), pg.map);
+    const int32_t page = clamp_page(__builtin_amdgcn_readlane(w_cur, win.lane(e)), pg.map);
     return ((int64_t)page << pg.map.shift) + ((t * kTile) & ((1 << pg.map.shift) - 1));
   };
 

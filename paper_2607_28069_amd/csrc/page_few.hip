@@ -81,8 +81,8 @@ page_few_kernel(PageFewArgs a) {
   // entries [win, win + 64) of the request's page table and the 64 after them
   const int32_t* ptab = a.map.table + (int64_t)b * a.map.cap;
   auto entry = [&](int32_t i) { return ptab[clamp_entry(i, a.map)]; };
-  int32_t win = c0 >> a.map.shift;
-  int32_t w_cur = entry(win + lane), w_next = entry(win + 64 + lane);
+  PageWindow win = {c0 >> a.map.shift};
+  int32_t w_cur = entry(win.at + lane), w_next = entry(win.at + 64 + lane);
   // the new tokens this workgroup stores, [st0, st1), 2 KC threads each, and the page of this thread's first
   const int st0 = min(max(wc0 - ctx, 0), n_tok), st1 = min(max(wc1 - ctx, 0), n_tok);
   const int st_i = st0 + tid / (2 * KC);
@@ -90,12 +90,11 @@ page_few_kernel(PageFewArgs a) {
   // the row that slot k0 lies in: k0 uniform, a multiple of 16, never less than the one asked for before
   auto row_at = [&](int k0) -> int32_t {
     const int32_t i = k0 >> a.map.shift;
-    if (i >= win + 64) {
-      win += 64;
+    if (win.moves(i, 64)) {
       w_cur = w_next;
-      w_next = entry(win + 64 + lane);
+      w_next = entry(win.at + 64 + lane);
     }
-    const int32_t page = clamp_page(__builtin_amdgcn_readlane(w_cur, i - win), a.map);
+    const int32_t page = clamp_page(__builtin_amdgcn_readlane(w_cur, win.lane(i)), a.map);
     return (page << a.map.shift) + (k0 & ((1 << a.map.shift) - 1));
   };
 

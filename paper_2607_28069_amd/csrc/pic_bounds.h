@@ -5,7 +5,8 @@
 //
 // The functions are __host__ __device__: the kernels call them, and the CPU emulation of the
 // launches that the sanitizer tests build (AddressSanitizer, UndefinedBehaviorSanitizer) calls
-// the same code on host buffers of the exact sizes.
+// the same code on host buffers of the exact sizes.  (Rows of a paged cache the kernels find through a
+// PageWindow, the emulation by page_row; that the two agree is a test of its own.)
 #pragma once
 
 #include <stdint.h>
@@ -91,7 +92,21 @@ struct PageMap {
 // Entry i of a request's page table, as a page to read: clamped into the table and the pages.
 PIC_HD int32_t clamp_entry(int32_t i, const PageMap& m) { return clamp_i32(i, 0, m.cap - 1); }
 PIC_HD int32_t clamp_page(int32_t page, const PageMap& m) { return clamp_i32(page, 0, m.n_pages - 1); }
-// The row `slot` of request b is read from (slot >= 0).
+// A wave's view of its request's page table as its keys go by: lane j of one register holds entry at + j, of
+// another one entry at + step + j, loaded a window ahead.  The kernels walk it with these two and take entry i out of
+// lane lane(i).
+struct PageWindow {
+  int32_t at;
+  // Entry i is the next one asked for, no more than `step` past the last one.  True: the window has moved on by step
+  // (the second register becomes the first, and is loaded anew).
+  PIC_HD bool moves(int32_t i, int32_t step) {
+    if (i < at + step) return false;
+    at += step;
+    return true;
+  }
+  PIC_HD int32_t lane(int32_t i) const { return i - at; }
+};
+// The row `slot` of request b is read from (slot >= 0), found without a window.
 PIC_HD int64_t page_row(const PageMap& m, int32_t b, int32_t slot) {
   const int32_t page = clamp_page(m.table[(int64_t)b * m.cap + clamp_entry(slot >> m.shift, m)], m);
   return ((int64_t)page << m.shift) + (slot & ((1 << m.shift) - 1));
@@ -168,6 +183,29 @@ PIC_HD RangeCandidates suffix_range_candidates(int64_t tiles_total, int32_t tile
   r.lo = mean > least ? mean : least;
   r.step = ceil_div(r.top > r.lo ? r.top - r.lo : 1, kDecodeDealt - 1);
   return r;
+}
+// Workgroup `block` of a dealt launch, whose `total` workgroups are shared out to the XCDs in neighbours: its request,
+// kv head, key range and tile of query rows (the last first), and the partials' tokens of the requests before.
+// Request b has wgs(b) = heads * ranges(b) * row_tiles(b) workgroups.  False: none is left for it.
+struct DealtBlock {
+  int32_t b, g, split, mt, ranges, row_tiles, first;
+};
+template <typename W, typename R, typename M, typename T>
+PIC_HD bool dealt_block(int32_t block, int32_t xcds, int32_t total, W wgs, R ranges, M row_tiles, T tokens, DealtBlock& x) {
+  const int32_t per = (total + xcds - 1) / xcds, at = block / xcds;
+  int32_t in_b = (block % xcds) * per + at;
+  if (at >= per || in_b >= total) return false;
+  x.first = 0;
+  for (x.b = 0; in_b >= wgs(x.b); ++x.b) {
+    in_b -= wgs(x.b);
+    x.first += ranges(x.b) * tokens(x.b);
+  }
+  x.ranges = ranges(x.b);
+  x.row_tiles = row_tiles(x.b);
+  x.mt = x.row_tiles - 1 - in_b % x.row_tiles;
+  x.split = (in_b / x.row_tiles) % x.ranges;
+  x.g = in_b / (x.row_tiles * x.ranges);
+  return true;
 }
 // ceil(u / c) for 0 <= u <= 2^24, 1 <= c, inv ~ 1 / c: a float32 quotient, off by one at most, put right
 PIC_HD int32_t ceil_div24(int32_t u, int32_t c, float inv) {

@@ -342,19 +342,19 @@ prefill_bf16_kernel(PrefillArgs a) {
       const int32_t m = row_tiles(d.tok, a.n_rep), wgs = d.n * m * a.n_kv_heads;   // lane b: workgroups of request b
       int total = 0;
       for (int i = 0; i < a.batch; ++i) total += __builtin_amdgcn_readlane(wgs, i);
-      const int per = (total + kNumXcd - 1) / kNumXcd;
-      int in_b = (w % kNumXcd) * per + at;   // (per <= per_xcd)
-      if (at >= per || in_b >= total) return;
-      first = 0;
-      for (b = 0; in_b >= __builtin_amdgcn_readlane(wgs, b); ++b) {
-        in_b -= __builtin_amdgcn_readlane(wgs, b);
-        first += __builtin_amdgcn_readlane(d.n, b) * __builtin_amdgcn_readlane(d.tok, b);
-      }
-      n_ranges = __builtin_amdgcn_readlane(d.n, b);
-      m_tiles_b = __builtin_amdgcn_readlane(m, b);
-      mt = m_tiles_b - 1 - in_b % m_tiles_b;
-      split = (in_b / m_tiles_b) % n_ranges;
-      g = in_b / (m_tiles_b * n_ranges);
+      // (the launch has a.n_wg workgroups rounded up to the XCDs: total or more)
+      DealtBlock x;
+      if (!dealt_block(w, kNumXcd, total, [&](int i) { return __builtin_amdgcn_readlane(wgs, i); },
+                       [&](int i) { return __builtin_amdgcn_readlane(d.n, i); }, [&](int i) { return __builtin_amdgcn_readlane(m, i); },
+                       [&](int i) { return __builtin_amdgcn_readlane(d.tok, i); }, x))
+        return;
+      b = x.b;
+      g = x.g;
+      mt = x.mt;
+      split = x.split;
+      n_ranges = x.ranges;
+      m_tiles_b = x.row_tiles;
+      first = x.first;
     } else if (logical >= a.n_wg) {
       return;
     }
@@ -462,27 +462,27 @@ prefill_bf16_kernel(PrefillArgs a) {
   // as the table gives it (a tile's rows lie in 4 pages at most, so a window can move on by 56 before
   // its last entries are needed); from this wave's first rows on
   constexpr int kWindow = 56;
-  int32_t pwin = 0, w_next = 0;
+  PageWindow pwin = {0};
+  int32_t w_next = 0;
   uint32_t w_cur = 0;
   auto entry = [&](int32_t i) { return a.map.table[(int64_t)b * a.map.cap + clamp_entry(i, a.map)]; };
   auto page_bytes = [&](int32_t page) { return ((uint32_t)clamp_page(page, a.map) << a.map.shift) * kRowBytes; };
   if constexpr (kPages) {
-    pwin = (t0 * kKeys + kRowsPerLoad * wave) >> a.map.shift;
-    w_next = entry(pwin + kWindow + lane);
-    w_cur = page_bytes(entry(pwin + lane));
+    pwin.at = (t0 * kKeys + kRowsPerLoad * wave) >> a.map.shift;
+    w_next = entry(pwin.at + kWindow + lane);
+    w_cur = page_bytes(entry(pwin.at + lane));
   }
   // pages: where the rows that this wave's load instructions of global tile T move lie, in bytes (T one
   // more each time)
   auto tile_rows = [&](int T, uint32_t (&pr)[kLoadSteps]) {   // T uniform
-    if (((T * kKeys + kRowsPerLoad * wave) >> a.map.shift) >= pwin + kWindow) {
-      pwin += kWindow;
+    if (pwin.moves((T * kKeys + kRowsPerLoad * wave) >> a.map.shift, kWindow)) {
       w_cur = page_bytes(w_next);
-      w_next = entry(pwin + kWindow + lane);
+      w_next = entry(pwin.at + kWindow + lane);
     }
 #pragma unroll
     for (int i = 0; i < kLoadSteps; ++i) {
       const int32_t slot = T * kKeys + kRowsPerLoad * (kWaves * i + wave);
-      const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)w_cur, (slot >> a.map.shift) - pwin);
+      const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)w_cur, pwin.lane(slot >> a.map.shift));
       pr[i] = at + (uint32_t)(slot & ((1 << a.map.shift) - 1)) * kRowBytes;
     }
   };
