@@ -265,7 +265,7 @@ PIC_API pic_status pic_page_blocks(const pic_pages* pages, int32_t batch, const 
       const int32_t slot = b.dst_slot + t, in_page = slot % P;
       pic_block& o = out[n++];
       o.request = 0;
-      o.src_token = b.src_token + t;
+      o.src_token = (int32_t)((uint32_t)b.src_token + (uint32_t)t);   // (past INT32_MAX: negative, so in no pool)
       o.dst_slot = page_table[(int64_t)b.request * pages->table_cap + slot / P] * P + in_page;
       o.n_tokens = std::min(b.n_tokens - t, P - in_page);
       o.delta = b.delta;
