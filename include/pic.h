@@ -464,7 +464,8 @@ typedef struct {
    pic_page_blocks rewrites gather blocks (pic_plan_layout / pic_plan_frontier) into blocks of the
    paged buffers, cut where pages end: request 0, dst_slot the row of the page.  PIC_ERR_RANGE for a
    block outside the table or over an entry that is no page, PIC_ERR_CAPACITY with *n_out the blocks
-   needed when out_cap is too small. */
+   needed when out_cap is too small.  (No call attends at pic_plan_frontier's inline positions over
+   pages: the documents of such a layout can be composed there, its inline tokens not computed.) */
 pic_status pic_page_grow(const pic_pages* pages, int32_t batch, int32_t* refs, int32_t* page_table,
                          const int32_t* len, const int32_t* new_len, int32_t* pairs, int32_t pair_cap,
                          int32_t* n_pairs);
@@ -524,9 +525,10 @@ pic_status pic_page_suffix_attn_rope(const pic_model* model, const pic_pages* pa
 
 /* ---- 5d. decode over pages ----
    pic_decode_attn on a paged cache: stores the new token at slot p = base_len[b] + step and attends
-   over slots [0, p]; split over the context and joined alike.  On bf16 pages probabilities keep 16 bits
+   over slots [0, p].  On bf16 pages split over the context and joined alike; probabilities keep 16 bits
    where pic_decode_attn rounds them to 8, so outputs carry little more than their own rounding, and the
-   ranges of a split launch are those of each request's own keys.
+   ranges of a split launch are those of each request's own keys.  On float32 pages one workgroup serves a
+   (request, kv head) whatever the length, and n_splits is ignored, as in pic_decode_attn.
      page_table [device, batch x table_cap]
      base_len   [device, batch]   clamped to max_base_len; a negative one marks padding of the batch:
                                   nothing of that request is read or stored, its out rows are left untouched

@@ -147,10 +147,10 @@ int32_t decode_cap_splits(int64_t splits, int32_t max_len) {
 //    and 286 / 245; of 4K keys 264 129 / 101 and 97 / 98, 384 139 / 135 and 127 / 134, hence the later line);
 //  * beyond, none: uneven contexts even out by themselves (400 pairs of 4K keys 139 / 144, 520 205 / 185
 //    but uneven 138 / 166, 776 281 / 267 but uneven 209 / 238).
-// Head_dim 64 keeps up to four workgroups on a compute unit, which evens that out by itself (384
-// pairs: 120 us whole, 137 us in 4), and each has half the bytes in flight: there the count is rounded
-// up where rounding down leaves under 200 workgroups or one range (down / up, 4K keys, and 16K keys
-// half as long at the shortest: 88 pairs 24.7 / 23.6 and 72 / 69 us, 136 41.9 / 35.1 and 131 / 101, 192
+// Head_dim 64 loses by 4 ranges past 256 pairs (384: 120 us whole, 137 us in 4), and a workgroup there has
+// half the bytes in flight (two share a compute unit, as at 128: the kernels are compiled for that).  Up to 256
+// the count is rounded up where rounding down leaves under 200 workgroups or one range (down / up, 4K keys, and
+// 16K keys half as long at the shortest: 88 pairs 24.7 / 23.6 and 72 / 69 us, 136 41.9 / 35.1 and 131 / 101, 192
 // 41.1 / 39.7 and 131 / 111, 224 45.2 / 43.3 and 134 / 122), and down elsewhere (72 pairs 18.6 / 19.4
 // and 51 / 56, 104 27.0 / 26.6 and 74 / 74, 120 27.5 / 28.0 and 76 / 78).
 int32_t decode_bf16_auto_splits(const AttnShape& s, int32_t max_len) {
