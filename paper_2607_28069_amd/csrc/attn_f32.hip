@@ -355,10 +355,9 @@ __global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t
   __syncthreads();
   for (int c = tid; c < ROWS * (HD / 4); c += 64 * W) {
     const int rr = c / (HD / 4), d = 4 * (c % (HD / 4));
-    const int r = row0 + rr;
-    if (r >= M) continue;
-    const int tok = r / n_rep;
-    if (pos_of(tok) < 0) continue;   // a token without a position: its row is left untouched
+    const int r = row0 + rr, tok = r / n_rep;
+    const bool live = r < M && pos_of(tok) >= 0;   // (a token without a position: its row is left untouched)
+    if (!kPages && !live) continue;
     float m = -INFINITY;
 #pragma unroll
     for (int w = 0; w < W; ++w) m = fmaxf(m, m_lds[w * ROWS + rr]);
@@ -372,22 +371,39 @@ __global__ void __launch_bounds__(64 * W) attn_f32_kernel(F32AttnArgs a, int32_t
       den += wt * lw;
       acc += wt * *reinterpret_cast<const f32x4*>(o_lds + (w * ROWS + rr) * LROW + d);
     }
-    // pages: a probability or weight may be 0 in 32 bits where the softmax's is not; values that are not finite then
-    // count without (where the scores are finite: else the outputs are NaN anyway)
-    if (kPages && !(fabsf(acc[0]) + fabsf(acc[1]) + fabsf(acc[2]) + fabsf(acc[3]) < INFINITY) && fabsf(den) < INFINITY) {
-      f32x4 odd = {};
-      const int end = (int)pos_of(tok);
-#pragma unroll 4
-      for (int key = 0; key <= end; ++key) {
-        const float* row = key < fresh ? Vg + page_row(pg.map, b, key) * HD : a.v_new + new0 + (int64_t)(key - fresh) * new_stride;
-        const f32x4 v = *reinterpret_cast<const f32x4*>(row + d);
+    if constexpr (kPages) {
+      // a probability or weight may be 0 in 32 bits where the softmax's is not; values that are not finite then count
+      // without (where the scores are finite: else the outputs are NaN anyway)
+      const bool odd = live && !(fabsf(acc[0]) + fabsf(acc[1]) + fabsf(acc[2]) + fabsf(acc[3]) < INFINITY) && fabsf(den) < INFINITY;
+      if (__any(odd)) {
+        f32x4 sum = {};
+        auto add = [&](f32x4 v) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!(fabsf(v[e]) < INFINITY)) sum[e] += v[e];
+        };
+        // cached values, which every row sees: a wave's groups of HD / 4 lanes share the keys, eight rows a lane on their
+        // way at once (past the last: that one again, which changes no such sum)
+        constexpr int kLanes = HD / 4, kAhead = 8;
+        for (int key0 = lane / kLanes; key0 < fresh; key0 += kAhead * (64 / kLanes)) {
+          f32x4 v[kAhead];
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i)
+            v[i] = *reinterpret_cast<const f32x4*>(Vg + page_row(pg.map, b, min(key0 + i * (64 / kLanes), fresh - 1)) * HD + d);
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) add(v[i]);
+        }
+#pragma unroll
+        for (int off = kLanes; off < 64; off <<= 1)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], off, 64);
+        for (int i = 0; live && i <= tok; ++i)   // and the new tokens' up to the row's own
+          add(*reinterpret_cast<const f32x4*>(a.v_new + new0 + i * new_stride + d));
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (!(fabsf(v[e]) < INFINITY)) odd[e] += v[e];
+          if (!(fabsf(sum[e]) < INFINITY)) acc[e] = sum[e];
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (!(fabsf(odd[e]) < INFINITY)) acc[e] = odd[e];
+      if (!live) continue;
     }
     *reinterpret_cast<f32x4*>(a.out + ((lb * n_q + tok) * Hq + g * n_rep + (r - tok * n_rep)) * HD + d) = acc / den;
   }

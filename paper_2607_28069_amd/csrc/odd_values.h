@@ -32,9 +32,8 @@ __device__ __forceinline__ void odd_partials(float (&o)[N], int n, X x) {
     if (!(fabsf(sum[e]) < INFINITY)) o[e] = sum[e];
 }
 // The values of a row's 8 head dims that are not finite, into sum.
-__device__ __forceinline__ void add_odd(const bf16_t* row8, float (&sum)[8]) {
-  const uint4 w4 = *reinterpret_cast<const uint4*>(row8);
-  const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+__device__ __forceinline__ void add_odd(uint4 row8, float (&sum)[8]) {
+  const uint32_t w[4] = {row8.x, row8.y, row8.z, row8.w};
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float v = __builtin_bit_cast(float, e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
@@ -42,11 +41,22 @@ __device__ __forceinline__ void add_odd(const bf16_t* row8, float (&sum)[8]) {
   }
 }
 // By a whole wave: the sum of those of head dims 8 c .. + 7, c = lane % KC, over keys [k0, k1) (row(key): where a key's
-// values lie); 0 where all are finite.
+// values lie); 0 where all are finite.  Eight rows a lane are on their way at once; keys past the last are that one
+// again, which changes no such sum.
 template <int KC, typename Row>
 __device__ __forceinline__ void odd_values(Row row, int k0, int k1, float (&sum)[8]) {
+  constexpr int kAhead = 8, kStep = 64 / KC;
   const int lane = threadIdx.x & 63;
-  for (int key = k0 + lane / KC; key < k1; key += 64 / KC) add_odd(row(key) + 8 * (lane % KC), sum);
+  for (int key0 = k0 + lane / KC; key0 < k1; key0 += kAhead * kStep) {
+    const bf16_t* at[kAhead];
+    uint4 x[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) at[i] = row(min(key0 + i * kStep, k1 - 1)) + 8 * (lane % KC);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) x[i] = *reinterpret_cast<const uint4*>(at[i]);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) add_odd(x[i], sum);
+  }
 #pragma unroll
   for (int off = KC; off < 64; off <<= 1)
 #pragma unroll

@@ -396,7 +396,8 @@ page_few_kernel(PageFewArgs a) {
   if (__any((odd_new || any_odd(o)) && fabsf(den) < INFINITY)) {
     float v[8] = {};
     odd_values<KC>([&](int key) { return Vg + page_row(a.map, b, key) * HD; }, wc0, min(wc1, ctx), v);
-    for (int key = max(wc0, ctx); key < wc1 && key <= ctx + r / n_rep; ++key) add_odd(Vn + (key - ctx) * new_stride + md, v);
+    for (int key = max(wc0, ctx); key < wc1 && key <= ctx + r / n_rep; ++key)
+      add_odd(*reinterpret_cast<const uint4*>(Vn + (key - ctx) * new_stride + md), v);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (!(fabsf(v[e]) < INFINITY)) o[e] = v[e];
