@@ -548,6 +548,129 @@ pic_status pic_page_decode_attn_rope(const pic_model* model, const pic_pages* pa
                                      int32_t max_abs_delta, float scale, int32_t n_splits, void* out,
                                      void* workspace, size_t ws_bytes, void* stream);
 
+/* ---- 5e. decode and suffix prefill over pages for batches that share prefixes ----
+   pic_page_decode_attn and pic_page_suffix_attn where requests hold the same K/V in their first slots (forks of one
+   request, questions about the same documents): each group of them reads its shared slots once, for all of its
+   requests together, instead of once per request.
+   The requests of a group are neighbours in the batch: group i holds requests [group_start[i], group_start[i + 1])
+   and shares slots [0, shared_len[i]), read through the page table row of its first request.  That request may be padding of
+   the batch (one that holds the prefix): nothing else of it is read then.  The other requests' tables must name pages
+   that hold the same there (pic_page_fork's do).  A request whose new tokens come before the end of the shared slots sees its own
+   slots only, [0, p], as always; the last shared_len[i] % 64 shared slots are read by each request.  Requests in no group
+   share nothing.
+     n_groups                    >= 1
+     max_group                   bound on the requests of a group: those past it in their group share nothing
+     max_len                     bound on shared_len (clamped to it); <= table_cap * page_tokens
+     group_start [device, n_groups + 1]  increasing; NULL: one group, the whole batch (n_groups 1)
+     shared_len  [device, n_groups]
+     workspace                   pic_page_shared_workspace_bytes(...) bytes for the same model, groups, batch and n_new
+                                 (decode: 1) and max_ctx (decode: max_base_len + step)
+   (the other arguments, padding, what is stored and what is not finite as for pic_page_suffix_attn and
+   pic_page_decode_attn; queries and keys rotated; n_suffix * Hkv below 2^24.)  bf16 probabilities keep 16 bits, so
+   outputs carry little more than their own rounding.  Last bits depend on the batch and on the bounds, which set the
+   key ranges of the launch, never on the lengths of other requests.  On float32 pages the calls are those two, request by
+   request, and need no workspace. */
+typedef struct {
+  int32_t n_groups;
+  int32_t max_group;
+  int32_t max_len;
+} pic_shared;
+size_t pic_page_shared_workspace_bytes(const pic_model* model, const pic_shared* shared, int32_t batch, int32_t n_new,
+                                       int32_t max_ctx);
+pic_status pic_page_shared_suffix_attn(const pic_model* model, const pic_pages* pages, const pic_shared* shared,
+                                       const void* q, const void* k_suf, const void* v_suf, void* pages_k,
+                                       void* pages_v, const int32_t* page_table, int32_t batch,
+                                       const int32_t* group_start, const int32_t* shared_len, const int32_t* ctx_len,
+                                       int32_t max_ctx, const int32_t* n_valid, int32_t n_suffix, float scale, void* out,
+                                       void* workspace, size_t ws_bytes, void* stream);
+pic_status pic_page_shared_decode_attn(const pic_model* model, const pic_pages* pages, const pic_shared* shared,
+                                       const void* q, const void* k_new, const void* v_new, void* pages_k,
+                                       void* pages_v, const int32_t* page_table, int32_t batch,
+                                       const int32_t* group_start, const int32_t* shared_len, const int32_t* base_len,
+                                       int32_t step, int32_t max_base_len, float scale, void* out, void* workspace,
+                                       size_t ws_bytes, void* stream);
+
+/* ---- 5f. page bookkeeping on the device ----
+   For loops that do not come back to the host at every page's end (a captured decode loop): pic_page_grow with its
+   arrays on the device, enqueued on `stream`, and pic_page_copy with its pairs there.  Tables and pairs come out as
+   pic_page_grow's do, entry for entry; the two may take turns on the same state, copied over.
+   pic_page_grow_async makes requests ready to store the tokens that an attention call with the same base_len, offset (its
+   step), n_valid and n_new will store: slots [base_len[b] + offset, + n), n = n_new or n_valid[b] clamped to
+   [0, n_new]; a negative base_len is padding of the batch and left alone.
+     refs [n_pages], page_table [batch][table_cap]   device, updated in place
+     base_len [batch], n_valid [batch] or NULL       device
+     pairs  [device out, batch x 2]  the (source, destination) pairs first, the rest -1
+     ready  [device out, batch]      base_len for the attention call: that given, or, where the call failed, -1 for
+                                     every request, so that nothing is stored into pages that others share
+     result [device out, 3]          a status (PIC_OK; PIC_ERR_CAPACITY: free pages or table_cap do not suffice;
+                                     PIC_ERR_RANGE: an entry that is neither -1 nor a page with a reference, where a new
+                                     slot needs it; nothing is changed then), pairs, and pages taken (where too few were
+                                     free: needed)
+     workspace  pic_page_grow_workspace_bytes(...) bytes (0: bad arguments)
+   pic_page_copy_async copies every pair of the pair_cap ones whose pages both lie in [0, n_pages), as if at once: no page may
+   be written twice, or both read and written (not checked: such pages would hold a mixture). */
+size_t pic_page_grow_workspace_bytes(const pic_pages* pages, int32_t batch, int32_t n_new);
+pic_status pic_page_grow_async(const pic_pages* pages, int32_t batch, int32_t* refs, int32_t* page_table,
+                               const int32_t* base_len, int32_t offset, const int32_t* n_valid, int32_t n_new,
+                               int32_t* pairs, int32_t* ready, int32_t* result, void* workspace, size_t ws_bytes,
+                               void* stream);
+pic_status pic_page_copy_async(const pic_model* model, const pic_pages* pages, void* pages_k, void* pages_v,
+                               const int32_t* pairs, int32_t pair_cap, void* stream);
+
+/* ---- 6. new tokens before their attention: norms of queries and keys with the rotation ----
+   For models that normalise each query and key head before the rotation (Qwen3), and for rotations that the fused
+   calls do not cover: turns the rows of a layer's projections into what the attention calls take, in one pass.  For
+   token i < n of request b at position p = base_len[b] + offset + i (offset + i without base_len) and each head x:
+     y = x * w / sqrt(mean(x^2) + eps)                              (no weights: y = x)
+     out = rope_scale * R(p) y on elements [0, rope_dim), y on the others
+   in float32, rounded once (elements past 2^63 in magnitude overflow the sum of squares).
+     q_weight, k_weight   [device, n_layers x D] float32, or NULL: not normalised
+     rope_dim       elements that turn: 0 (all of them) or a multiple of 16 up to head_dim.  Pairs are those of
+                    model->rope_pairing within them: i and i + rope_dim / 2, or 2i and 2i + 1
+     rope_order     PIC_ROPE_ORDER_KEEP: elements stay in place.  PIC_ROPE_ORDER_PAIRS (rotate-half only, no
+                    effect on interleaved pairs): pair i at i and i + D / 2, where the other calls turn it, and
+                    the elements that do not turn, in order, in the places left.  Scores do not change by it, as queries
+                    and keys are laid out alike, and pic_rerotate_keys, pic_compose and the zero-copy calls, given a table
+                    whose frequencies past rope_dim / 2 are 0, turn such keys rightly
+     rope_scale     factor on the turned elements (pic_rope_yarn_freq's attention factor); 0 means 1
+     q, k, v        rows [n_layers][batch][n_new][heads][D], q_stride (k_stride, v_stride) elements from token to
+                    token (slices of one projection), a multiple of 16 bytes; 0: dense.  v is only moved.
+                    Each may be NULL: left out
+     q_out, k_out, v_out   dense; may be q, k, v themselves where those are dense
+     base_len       [device, batch] clamped to max_base_len; a negative one is padding of the batch.  NULL: positions
+                    from `offset` (documents being compiled; max_base_len is not used)
+     n_valid        [device, batch] tokens used, clamped to [0, n_new]; NULL: all.  Rows of padding are left untouched
+     table          pic_rope_table_init(_freq) for this model: frequency i in column i; NULL: no rotation
+     max_abs_delta  of the table; max_base_len + offset + n_new - 1 at least (PIC_ERR_RANGE) */
+typedef enum {
+  PIC_ROPE_ORDER_KEEP = 0,
+  PIC_ROPE_ORDER_PAIRS = 1
+} pic_rope_order;
+typedef struct {
+  const float* q_weight;
+  const float* k_weight;
+  float eps;
+  int32_t rope_dim;
+  int32_t rope_order;
+  float rope_scale;
+} pic_qk_norm;
+pic_status pic_qk_norm_rope(const pic_model* model, const pic_qk_norm* how, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t batch,
+                            const int32_t* base_len, int32_t max_base_len, int32_t offset, const int32_t* n_valid,
+                            int32_t n_new, const void* table, int32_t max_abs_delta, void* q_out, void* k_out,
+                            void* v_out, void* stream);
+
+/* Host helper: frequencies stretched for long contexts pair by pair (YaRN) for pic_rope_table_init_freq, from
+   theta_i = theta^(-2i/rope_dim): a pair that turns more than beta_fast times over original_max_position is kept, one
+   that turns less than beta_slow times divided by factor, and in between the two are blended linearly in i (from the
+   bounds rounded outwards).  Writes head_dim / 2 values to inv_freq [host], 0 past rope_dim / 2 (rope_dim 0: the
+   whole head), and 0.1 ln(factor) + 1 to attention_factor [host], which queries and keys are both multiplied by
+   (pic_qk_norm's rope_scale).  PIC_ERR_INVALID_ARG for a head_dim other than 64 or 128, factor < 1, beta_slow <= 0 or
+   beta_fast <= beta_slow; PIC_ERR_UNSUPPORTED for another rope_dim than a multiple of 16. */
+pic_status pic_rope_yarn_freq(int32_t head_dim, int32_t rope_dim, double theta, double factor,
+                              double original_max_position, double beta_fast, double beta_slow, double* inv_freq,
+                              double* attention_factor);
+
 /* ---- diagnostics ---- */
 const char* pic_status_string(pic_status status);
 /* Thread-local description of the last failure on this thread ("" if none). */

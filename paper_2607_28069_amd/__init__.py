@@ -33,7 +33,10 @@ EXPORTS = ("pic_plan_layout", "pic_plan_frontier", "pic_rope_table_bytes", "pic_
            "pic_last_error",
            "pic_decode_auto_splits", "pic_decode_attn_noalloc",
            "pic_page_grow", "pic_page_fork", "pic_page_free", "pic_page_compact", "pic_page_blocks", "pic_page_copy",
-           "pic_page_suffix_attn", "pic_page_suffix_attn_rope", "pic_page_decode_attn", "pic_page_decode_attn_rope")
+           "pic_page_suffix_attn", "pic_page_suffix_attn_rope", "pic_page_decode_attn", "pic_page_decode_attn_rope",
+           "pic_page_shared_workspace_bytes", "pic_page_shared_suffix_attn", "pic_page_shared_decode_attn",
+           "pic_page_grow_workspace_bytes", "pic_page_grow_async", "pic_page_copy_async",
+           "pic_qk_norm_rope", "pic_rope_yarn_freq")
 PIC_DECODE_SCRATCH_BYTES = 8 << 20
 
 
@@ -75,6 +78,35 @@ class Pages(ctypes.Structure):
     @classmethod
     def of(cls, n_pages, page_tokens, table_cap):
         return cls(int(n_pages), int(page_tokens), int(table_cap))
+
+
+class Shared(ctypes.Structure):
+    """pic_shared: n_groups groups of at most max_group neighbouring requests, which share at most max_len slots."""
+    _fields_ = [("n_groups", ctypes.c_int32), ("max_group", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+    @classmethod
+    def of(cls, n_groups, max_group, max_len):
+        return cls(int(n_groups), int(max_group), int(max_len))
+
+
+PIC_ROPE_ORDER_KEEP, PIC_ROPE_ORDER_PAIRS = 0, 1
+
+
+class QkNorm(ctypes.Structure):
+    """pic_qk_norm: norms of queries and keys (float32 weights [n_layers][D], None: not normalised) and the part of a
+    head that turns.  Holds on to the weights."""
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("rope_dim", ctypes.c_int32), ("rope_order", ctypes.c_int32), ("rope_scale", ctypes.c_float)]
+
+    @classmethod
+    def of(cls, q_weight, k_weight, eps=1e-6, rope_dim=0, rope_order="keep", rope_scale=1.0):
+        order = {"keep": PIC_ROPE_ORDER_KEEP, "pairs": PIC_ROPE_ORDER_PAIRS}.get(rope_order, rope_order)
+        for w in (q_weight, k_weight):
+            if w is not None and str(w.dtype) != "torch.float32":
+                raise ValueError("weights: float32 expected")
+        x = cls(_ptr(q_weight), _ptr(k_weight), float(eps), int(rope_dim), order, float(rope_scale))
+        x.weights = (q_weight, k_weight)
+        return x
 
 
 BLOCK_DTYPE = np.dtype([("request", np.int32), ("src_token", np.int32), ("dst_slot", np.int32),
@@ -136,6 +168,17 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "pic_page_decode_attn_rope": (ctypes.c_int, [MP, PP, P, P, P, P, P, P, I32, P, I32, I32, P, I32, F, I32, P, P,
                                                      SZ, P]),
     }
+    SP, NP, D = ctypes.POINTER(Shared), ctypes.POINTER(QkNorm), ctypes.c_double
+    sig.update({
+        "pic_page_shared_workspace_bytes": (SZ, [MP, SP, I32, I32, I32]),
+        "pic_page_shared_suffix_attn": (ctypes.c_int, [MP, PP, SP, P, P, P, P, P, P, I32, P, P, P, I32, P, I32, F, P, P, SZ, P]),
+        "pic_page_shared_decode_attn": (ctypes.c_int, [MP, PP, SP, P, P, P, P, P, P, I32, P, P, P, I32, I32, F, P, P, SZ, P]),
+        "pic_page_grow_workspace_bytes": (SZ, [PP, I32, I32]),
+        "pic_page_grow_async": (ctypes.c_int, [PP, I32, P, P, P, I32, P, I32, P, P, P, P, SZ, P]),
+        "pic_page_copy_async": (ctypes.c_int, [MP, PP, P, P, P, I32, P]),
+        "pic_qk_norm_rope": (ctypes.c_int, [MP, NP, P, I64, P, I64, P, I64, I32, P, I32, I32, P, I32, P, I32, P, P, P, P]),
+        "pic_rope_yarn_freq": (ctypes.c_int, [I32, I32, D, D, D, D, D, P, P]),
+    })
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = res, args
@@ -550,6 +593,110 @@ def pic_page_decode_attn_rope(model: Model, pages: Pages, q, k_new, v_new, pages
     _check(load().pic_page_decode_attn_rope(ctypes.byref(model), ctypes.byref(pages), *a, tab, int(batch), lens, int(step),
                                             int(max_base_len), rt, int(max_abs_delta), float(scale), int(n_splits), o, ws,
                                             _ws_bytes(workspace), st))
+
+
+def pic_page_shared_workspace_bytes(model: Model, shared: Shared, batch, n_new, max_ctx) -> int:
+    """For a decode: n_new 1, max_ctx max_base_len + step."""
+    return load().pic_page_shared_workspace_bytes(ctypes.byref(model), ctypes.byref(shared), int(batch), int(n_new), int(max_ctx))
+
+
+def pic_page_shared_suffix_attn(model: Model, pages: Pages, shared: Shared, q, k_suf, v_suf, pages_k, pages_v, page_table,
+                                batch, group_start, shared_len, ctx_len, max_ctx, n_suffix, out, workspace=None, n_valid=None,
+                                scale=0.0, stream=None):
+    """group_start: device int32 [n_groups + 1], or None (one group); shared_len: device int32 [n_groups]."""
+    (*a, tab, gs, sl, lens, nv, o, ws), st = _on_device((q, k_suf, v_suf, pages_k, pages_v, page_table, group_start, shared_len,
+                                                         ctx_len, n_valid, out, workspace), stream)
+    _check(load().pic_page_shared_suffix_attn(ctypes.byref(model), ctypes.byref(pages), ctypes.byref(shared), *a, tab, int(batch),
+                                              gs, sl, lens, int(max_ctx), nv, int(n_suffix), float(scale), o, ws,
+                                              _ws_bytes(workspace), st))
+
+
+def pic_page_shared_decode_attn(model: Model, pages: Pages, shared: Shared, q, k_new, v_new, pages_k, pages_v, page_table,
+                                batch, group_start, shared_len, base_len, step, max_base_len, out, workspace=None, scale=0.0,
+                                stream=None):
+    """group_start: device int32 [n_groups + 1], or None (one group); shared_len: device int32 [n_groups]."""
+    (*a, tab, gs, sl, lens, o, ws), st = _on_device((q, k_new, v_new, pages_k, pages_v, page_table, group_start, shared_len,
+                                                     base_len, out, workspace), stream)
+    _check(load().pic_page_shared_decode_attn(ctypes.byref(model), ctypes.byref(pages), ctypes.byref(shared), *a, tab, int(batch),
+                                              gs, sl, lens, int(step), int(max_base_len), float(scale), o, ws,
+                                              _ws_bytes(workspace), st))
+
+
+def pic_page_grow_workspace_bytes(pages: Pages, batch, n_new) -> int:
+    return load().pic_page_grow_workspace_bytes(ctypes.byref(pages), int(batch), int(n_new))
+
+
+def _device_i32(t, n, name):
+    if t is not None and (str(t.dtype) != "torch.int32" or t.numel() != n):
+        raise ValueError(f"{name}: {n} int32 entries expected, got {t.numel()} of {t.dtype}")
+
+
+def pic_page_grow_async(pages: Pages, batch, refs, page_table, base_len, n_new, pairs, ready, result, workspace, n_valid=None,
+                        offset=0, stream=None):
+    """pic_page_grow on the device, for the tokens that an attention call with these base_len, offset, n_valid and n_new
+    stores: refs [n_pages] and page_table [batch][table_cap] are updated, pairs [batch][2], ready [batch] (base_len for that
+    call, -1 where this one fails) and result [3] (status, pairs, pages taken) written; device int32 tensors."""
+    for t, n, name in ((refs, pages.n_pages, "refs"), (page_table, batch * pages.table_cap, "page_table"),
+                       (base_len, batch, "base_len"), (n_valid, batch, "n_valid"), (pairs, 2 * batch, "pairs"),
+                       (ready, batch, "ready"), (result, 3, "result")):
+        _device_i32(t, n, name)
+    (rf, tab, lens, nv, pr, rd, rs, ws), st = _on_device((refs, page_table, base_len, n_valid, pairs, ready, result, workspace),
+                                                         stream)
+    _check(load().pic_page_grow_async(ctypes.byref(pages), int(batch), rf, tab, lens, int(offset), nv, int(n_new), pr, rd, rs, ws,
+                                      _ws_bytes(workspace), st))
+
+
+def pic_page_copy_async(model: Model, pages: Pages, pages_k, pages_v, pairs, pair_cap, stream=None):
+    """pairs: device int32 [pair_cap][2] (source, destination) pages; entries that are no pages are skipped."""
+    (k, v, pr), st = _on_device((pages_k, pages_v, pairs), stream)
+    _check(load().pic_page_copy_async(ctypes.byref(model), ctypes.byref(pages), k, v, pr, int(pair_cap), st))
+
+
+def _token_rows(t, heads, head_dim, name):
+    """(address, elements from token to token) of rows [..., heads, head_dim] on the current device, dense within a token
+    and one step from token to token: a dense tensor or a slice of a wider row."""
+    if t is None:
+        return None, 0
+    if t.dim() < 2 or t.shape[-1] != head_dim or t.shape[-2] != heads:
+        raise ValueError(f"{name}: [..., {heads}, {head_dim}] expected, got {tuple(t.shape)}")
+    step = heads * head_dim
+    if not t.is_contiguous():
+        if t.stride(-1) != 1 or (heads > 1 and t.stride(-2) != head_dim):
+            raise ValueError(f"{name}: a token's heads must be dense")
+        span = None   # of the token dimensions met so far, innermost first
+        for size, stride in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):
+            if size == 1:
+                continue
+            if span is None:
+                step = stride
+            elif stride != span:
+                raise ValueError(f"{name}: tokens must lie one step apart")
+            span = size * stride
+    if not t.is_cuda:
+        raise ValueError("device buffer expected: got a host tensor")
+    import torch
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} on device {t.get_device()}, the current one is {torch.cuda.current_device()}")
+    return t.data_ptr(), step
+
+
+def pic_qk_norm_rope(model: Model, how: QkNorm, q, k, v, batch, n_new, table, max_abs_delta, q_out, k_out, v_out, base_len=None,
+                     max_base_len=0, offset=0, n_valid=None, stream=None):
+    """q [..., n_q_heads, D], k and v [..., n_kv_heads, D] (tokens dense or a step apart; None: left out) to dense q_out, k_out,
+    v_out: heads normalised and turned to positions base_len[b] + offset + i."""
+    hq, hkv, d = model.n_q_heads, model.n_kv_heads, model.head_dim
+    (lens, nv, tab, qo, ko, vo), st = _on_device((base_len, n_valid, table, q_out, k_out, v_out), stream)
+    _check(load().pic_qk_norm_rope(ctypes.byref(model), ctypes.byref(how), *_token_rows(q, hq, d, "q"),
+                                   *_token_rows(k, hkv, d, "k"), *_token_rows(v, hkv, d, "v"), int(batch), lens,
+                                   int(max_base_len), int(offset), nv, int(n_new), tab, int(max_abs_delta), qo, ko, vo, st))
+
+
+def pic_rope_yarn_freq(head_dim, theta, factor, original_max_position, beta_fast=32.0, beta_slow=1.0, rope_dim=0):
+    """(frequencies [head_dim / 2] for pic_rope_table_init_freq, attention factor for QkNorm.rope_scale)."""
+    out, scale = np.zeros(head_dim // 2, np.float64), ctypes.c_double(0.0)
+    _check(load().pic_rope_yarn_freq(int(head_dim), int(rope_dim), float(theta), float(factor), float(original_max_position),
+                                     float(beta_fast), float(beta_slow), out.ctypes.data, ctypes.addressof(scale)))
+    return out, scale.value
 
 
 def pic_status_string(status: int) -> str:

@@ -17,8 +17,9 @@ LIB = os.path.join(PKG, "libpic.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
-SOURCES = ["pic_api.cpp", "pic_pages.cpp", "pic_plan.cpp", "rope_compose.hip", "attn_f32.hip", "prefill_bf16.hip",
-           "decode_bf16.hip", "page_decode.hip", "page_few.hip", "page_copy.hip"]
+SOURCES = ["pic_api.cpp", "pic_pages.cpp", "pic_plan.cpp", "pic_shared.cpp", "pic_grow.cpp", "pic_tokens.cpp", "rope_compose.hip",
+           "attn_f32.hip", "prefill_bf16.hip", "decode_bf16.hip", "page_decode.hip", "page_few.hip", "page_shared.hip",
+           "page_copy.hip", "page_grow.hip", "qk_norm.hip"]
 
 CFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17", "-fvisibility=hidden",

@@ -1,0 +1,265 @@
+// Page tables grown on the device from the requests' lengths, entry for entry what pic_page_grow does on the host, and
+// the page copies that it asks for.
+//
+// Growing is a few integers behind a chain of loads that wait for one another (lengths -> table entries -> reference
+// counts -> free pages -> the entries that take them), so one workgroup does it all: what
+// bounds it is that chain, and a second workgroup would add a launch or a wait between the two.  The order of the host's
+// loop (request by request, entry by entry) comes from prefix sums over the workgroup; where several entries hold the
+// same shared page, the k-th of them takes a page of its own if the page has more than k + 1 references, so the last
+// ones keep it.  Nothing is changed before it is known that everything fits.
+#include "pic_bounds.h"
+#include "pic_internal.h"
+
+namespace pic {
+namespace {
+
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+
+// Exclusive prefix sums of x over the workgroup, in thread order, and its total.  `sums` is reused by the next call.
+struct Scan {
+  int before, total;
+};
+__device__ __forceinline__ Scan scan(int x, int (&sums)[kWaves]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int in = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(in, d, 64);
+    if (lane >= d) in += y;
+  }
+  __syncthreads();   // (the last call's sums are read)
+  if (lane == 63) sums[wave] = in;
+  __syncthreads();
+  int before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    before += w < wave ? sums[w] : 0;
+    total += sums[w];
+  }
+  return {before + in - x, total};
+}
+
+// 1 workgroup.  workspace: first[batch + 1] (a request's first entry in the order), then of every entry in the order its
+// page where it is shared (shared[]), where in the order that was (at[]) and what becomes of it (take[]), and the free
+// pages in order (lowest[]).
+__global__ void __launch_bounds__(kThreads) page_grow_kernel(PageGrowArgs a, int32_t cap_entries) {
+  __shared__ int sums[kWaves];
+  __shared__ int bad_cap, bad_entry;
+  const int tid = threadIdx.x;
+  int32_t* first = a.workspace;
+  int32_t* shared = first + a.batch + 1;
+  int32_t* at = shared + cap_entries;
+  int32_t* take = at + cap_entries;
+  int32_t* lowest = take + cap_entries;
+  const int32_t P = 1 << a.shift;
+  if (tid == 0) bad_cap = bad_entry = 0;
+  __syncthreads();
+  // a request's new slots: [from, to), empty where it is left alone
+  auto slots = [&](int b, int64_t& from, int64_t& to) {
+    const int32_t base = a.base_len[b];
+    from = (int64_t)base + a.offset;
+    to = from + page_new_tokens(a.base_len, a.n_valid, b, a.n_new);
+    return to > from;
+  };
+  // 1. the entries each request's new slots lie in
+  int32_t entries = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kThreads) {
+    const int b = b0 + tid;
+    int n = 0;
+    int64_t from, to;
+    if (b < a.batch && slots(b, from, to)) {
+      const int64_t end = (to + P - 1) >> a.shift;
+      if (end > a.table_cap) bad_cap = 1;
+      else n = (int)(end - (from >> a.shift));
+    }
+    const Scan s = scan(n, sums);
+    if (b < a.batch) first[b] = entries + s.before;
+    entries += s.total;
+  }
+  if (tid == 0) first[a.batch] = entries;
+  __syncthreads();
+  bool fits = bad_cap == 0;   // (then at most cap_entries of them)
+  // entry e of the order: its request and place in the table
+  auto locate = [&](int e, int& b, int32_t& i, bool& partly) {
+    int lo = 0, hi = a.batch;   // first[lo] <= e < first[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= e) lo = mid;
+      else hi = mid;
+    }
+    b = lo;
+    const int64_t from = (int64_t)a.base_len[b] + a.offset;
+    i = (int32_t)(from >> a.shift) + (e - first[b]);
+    partly = e == first[b] && (from & (P - 1)) != 0;
+  };
+  // 2. what becomes of each: 0 kept, 1 takes a page, 2 shared (settled below)
+  int32_t n_shared = 0;
+  if (fits) {
+    for (int e0 = 0; e0 < entries; e0 += kThreads) {
+      const int e = e0 + tid;
+      int kind = 0;
+      int32_t page = -1;
+      if (e < entries) {
+        int b;
+        int32_t i;
+        bool partly;
+        locate(e, b, i, partly);
+        page = a.page_table[(int64_t)b * a.table_cap + i];
+        if (page == -1 && !partly) {
+          kind = 1;
+        } else if (page < 0 || page >= a.n_pages) {
+          bad_entry = 1;
+        } else {
+          const int32_t refs = a.refs[page];
+          if (refs < 1) bad_entry = 1;
+          kind = refs > 1 ? 2 : 0;
+        }
+        take[e] = kind;
+      }
+      const Scan s = scan(kind == 2, sums);
+      if (kind == 2) {
+        shared[n_shared + s.before] = page;
+        at[n_shared + s.before] = e;
+      }
+      n_shared += s.total;
+    }
+    __syncthreads();
+    fits = bad_entry == 0;
+  }
+  const bool known = fits;   // (bad tables: nothing is counted)
+  int32_t takes = 0, copies = 0, found = 0;
+  if (fits) {
+    for (int s = tid; s < n_shared; s += kThreads) {
+      const int32_t page = shared[s];
+      int rank = 0;
+      for (int k = 0; k < s; ++k) rank += shared[k] == page;
+      int b;
+      int32_t i;
+      bool partly;
+      locate(at[s], b, i, partly);
+      take[at[s]] = a.refs[page] - rank > 1 ? (partly ? 3 : 1) : 0;   // 3: and is copied
+    }
+    __syncthreads();
+    for (int e0 = 0; e0 < entries; e0 += kThreads) {
+      const Scan s = scan(e0 + tid < entries && take[e0 + tid] != 0, sums);
+      takes += s.total;
+    }
+    // 3. as many free pages, lowest first
+    for (int64_t p0 = 0; p0 < a.n_pages && found < takes; p0 += 4 * kThreads) {
+      const int64_t p = p0 + 4 * tid;
+      bool free_page[4];
+      int n = 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        free_page[u] = p + u < a.n_pages && a.refs[p + u] == 0;
+        n += free_page[u];
+      }
+      const Scan s = scan(n, sums);
+      int k = found + s.before;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (free_page[u]) {
+          if (k < takes) lowest[k] = (int32_t)(p + u);
+          ++k;
+        }
+      found += s.total;
+    }
+    __syncthreads();
+    fits = found >= takes;
+  }
+  // 4. the tables changed
+  if (fits) {
+    int32_t taken = 0;
+    for (int e0 = 0; e0 < entries; e0 += kThreads) {
+      const int e = e0 + tid;
+      const int kind = e < entries ? take[e] : 0;
+      const Scan s = scan(kind != 0, sums);
+      const Scan c = scan(kind == 3, sums);
+      if (kind != 0) {
+        int b;
+        int32_t i;
+        bool partly;
+        locate(e, b, i, partly);
+        int32_t* entry = a.page_table + (int64_t)b * a.table_cap + i;
+        const int32_t page = lowest[taken + s.before], old = *entry;
+        if (old >= 0) atomicSub(a.refs + old, 1);
+        a.refs[page] = 1;
+        *entry = page;
+        if (kind == 3) {
+          a.pairs[2 * (copies + c.before)] = old;
+          a.pairs[2 * (copies + c.before) + 1] = page;
+        }
+      }
+      taken += s.total;
+      copies += c.total;
+    }
+  }
+  for (int64_t i = 2 * (int64_t)copies + tid; i < 2 * (int64_t)a.batch; i += kThreads) a.pairs[i] = -1;
+  for (int b = tid; b < a.batch; b += kThreads) {
+    const int32_t base = a.base_len[b];
+    a.ready[b] = fits && base >= 0 ? base : -1;
+  }
+  if (tid == 0) {
+    a.result[0] = fits ? PIC_OK : bad_cap || known ? PIC_ERR_CAPACITY : PIC_ERR_RANGE;
+    a.result[1] = copies;
+    a.result[2] = known ? takes : 0;
+  }
+}
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Any grid, 256 threads.  Pairs come 64 at a time; a workgroup takes every gridDim.x-th piece (a pair in one stream) of
+// those that are pairs, so that a list without any costs one load.
+__global__ void __launch_bounds__(256) page_copy_listed_kernel(u32x4* k, u32x4* v, int64_t n_streams, int64_t stream16,
+                                                               int32_t page16, const int2* pairs, int32_t cap, int32_t n_pages) {
+  constexpr int kAhead = 4;
+  __shared__ int2 found[64];
+  const int lane = threadIdx.x & 63;
+  for (int64_t i0 = 0; i0 < cap; i0 += 64) {
+    const int2 mine = i0 + lane < cap ? pairs[i0 + lane] : make_int2(-1, -1);
+    const bool ok = mine.x >= 0 && mine.x < n_pages && mine.y >= 0 && mine.y < n_pages;
+    const uint64_t mask = __ballot(ok);
+    const int n = __popcll(mask);
+    if (n == 0) continue;   // (uniform: every wave holds the same 64)
+    __syncthreads();
+    if (ok && threadIdx.x < 64) found[__popcll(mask & ((uint64_t(1) << lane) - 1))] = mine;
+    __syncthreads();
+    for (int64_t at = blockIdx.x; at < n * 2 * n_streams; at += gridDim.x) {
+      const int32_t pair = (int32_t)(at / (2 * n_streams));
+      const int64_t st = at - pair * 2 * n_streams;
+      const int2 p = found[pair];
+      u32x4* base = st < n_streams ? k + st * stream16 : v + (st - n_streams) * stream16;
+      const u32x4* src = base + (int64_t)p.x * page16;
+      u32x4* dst = base + (int64_t)p.y * page16;
+      for (int i = threadIdx.x; i < page16; i += 256 * kAhead) {
+        u32x4 x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+          if (i + 256 * u < page16) x[u] = src[i + 256 * u];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+          if (i + 256 * u < page16) __builtin_nontemporal_store(x[u], dst + i + 256 * u);
+      }
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_page_grow(const PageGrowArgs& a, hipStream_t stream) {
+  const int64_t entries = page_grow_entries(1 << a.shift, a.table_cap, a.batch, a.n_new);
+  hipLaunchKernelGGL(page_grow_kernel, dim3(1), dim3(kThreads), 0, stream, a, (int32_t)entries);
+  return hipGetLastError();
+}
+
+hipError_t launch_page_copy_listed(void* pages_k, void* pages_v, int64_t n_streams, int64_t n_pages, int64_t page_bytes,
+                                   const int32_t* pairs, int32_t cap, hipStream_t stream) {
+  const int64_t page16 = page_bytes / 16;
+  const unsigned grid = (unsigned)std::min<int64_t>((int64_t)cap * 2 * n_streams, 2048);
+  hipLaunchKernelGGL(page_copy_listed_kernel, dim3(grid), dim3(256), 0, stream, static_cast<u32x4*>(pages_k),
+                     static_cast<u32x4*>(pages_v), n_streams, n_pages * page16, (int32_t)page16,
+                     reinterpret_cast<const int2*>(pairs), cap, (int32_t)n_pages);
+  return hipGetLastError();
+}
+
+}  // namespace pic

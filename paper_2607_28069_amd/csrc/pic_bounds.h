@@ -126,6 +126,39 @@ PIC_HD int32_t page_new_tokens(const int32_t* base_len, const int32_t* n_valid, 
   return n_valid ? clamp_len(n_valid[b], n_new) : n_new;
 }
 
+// ---- Requests that share a prefix: group i holds requests [start[i], start[i + 1]) (without starts, group 0 the whole
+// batch), the first max_group of them served together over slots [0, shared_len[i]) of its first request's pages.
+constexpr int32_t kSharedKeys = 64;   // the part that is served together ends with a whole tile
+struct SharedMap {
+  const int32_t* start = nullptr;   // [n_groups + 1]
+  const int32_t* len = nullptr;     // [n_groups]
+  int32_t n_groups = 0, max_group = 0, max_len = 0, batch = 0;
+
+  PIC_HD int32_t first(int32_t i) const { return start ? clamp_i32(start[i], 0, batch) : (i == 0 ? 0 : batch); }
+  PIC_HD int32_t requests(int32_t i) const {
+    const int32_t n = first(i + 1) - first(i);
+    return n < 0 ? 0 : (n < max_group ? n : max_group);
+  }
+  // Slots of group i that are served together.
+  PIC_HD int32_t slots(int32_t i) const { return clamp_len(len[i], max_len) & ~(kSharedKeys - 1); }
+  // The group whose prefix request b is served with, -1: none.  (Starts that do not increase: some group, or none.)
+  PIC_HD int32_t group_of(int32_t b) const {
+    int32_t lo = 0, hi = n_groups;   // first(lo) <= b < first(hi), once it is known that first(0) <= b
+    while (hi - lo > 1) {
+      const int32_t mid = lo + (hi - lo) / 2;
+      if (first(mid) <= b) lo = mid;
+      else hi = mid;
+    }
+    return b >= first(lo) && b - first(lo) < requests(lo) ? lo : -1;
+  }
+};
+// Slots of a request that its group serves, of a group that serves `slots` of them: whole tiles before the first new
+// token, at `ctx`.
+PIC_HD int32_t shared_part(int32_t slots, int32_t ctx) {
+  const int32_t whole = ctx & ~(kSharedKeys - 1);
+  return slots < whole ? slots : whole;
+}
+
 // ---- Split decode: the key ranges of a batch of uneven contexts ----
 // A split launch has n_splits workgroups per (request, kv head).  They are dealt to the requests
 // by length: request b of u_b units (kDecodeUnit keys each, the last one partial) gets

@@ -1,5 +1,5 @@
 // What the files of the C ABI share: the thread-local error, argument checks and launch decisions
-// (defined in pic_api.cpp).
+// (defined in pic_api.cpp, unless said).
 #pragma once
 
 #include "pic.h"
@@ -29,6 +29,7 @@ pic_status hip_status(hipError_t e, const char* what);
 bool aligned16(const void* p);
 pic_status check_ptr(const void* p, const char* name);
 pic_status check_model(const pic_model* m);
+pic_status check_pages(const pic_pages* pg);   // (defined in pic_pages.cpp)
 pic_status check_rows32(int64_t cache_cap, int64_t suffix_rows, int64_t pool_tokens);
 int32_t n_tables(const pic_model* m);
 AttnShape shape_of(const pic_model* m, int32_t batch, int32_t cache_cap, float scale);

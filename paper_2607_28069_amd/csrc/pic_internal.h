@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "pic.h"
 #include "pic_bounds.h"
 
@@ -257,5 +259,63 @@ hipError_t launch_decode_bf16(const AttnShape& s, const bf16_t* q, const bf16_t*
                               int32_t n_splits, bf16_t* out, void* workspace, size_t ws_bytes,
                               const float2* rope_table, int64_t table_stride, int32_t max_abs_delta,
                               bool interleaved, hipStream_t stream);
+
+// Attention of n_new new tokens per request over pages (see PageAttnArgs: base_len, n_valid, max_base, offset), where
+// groups of requests share a prefix.  bf16.  The plan: `row_blocks` blocks of 64 query rows per workgroup, key ranges of
+// a group's prefix and of a request's own slots, each with that many tiles of query rows.
+struct SharedPlan {
+  int32_t row_blocks = 1, prefix_splits = 1, own_splits = 1, prefix_row_tiles = 0, own_row_tiles = 0;
+  int64_t prefix_blocks = 0, own_blocks = 0;   // workgroups per layer
+  size_t ws_bytes = 0;
+};
+SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, int32_t max_ctx);
+hipError_t launch_shared_bf16_pages(const PageAttnArgs& a, const SharedMap& m, const SharedPlan& plan);
+
+// Norms of queries and keys with their rotation (rows of a token at q + token * q_stride and so on, token = (layer *
+// batch + request) * n_new + i; dense outputs).  Positions clamp_len(base_len[b], max_base) + offset + i, or offset + i
+// without base_len, all inside the table.
+struct QkNormArgs {
+  const void* q = nullptr;
+  const void* k = nullptr;
+  const void* v = nullptr;
+  void* q_out = nullptr;
+  void* k_out = nullptr;
+  void* v_out = nullptr;
+  int64_t q_stride = 0, k_stride = 0, v_stride = 0;   // elements
+  const float* q_weight = nullptr;   // [L][D]; NULL: not normalised
+  const float* k_weight = nullptr;
+  const int32_t* base_len = nullptr;
+  const int32_t* n_valid = nullptr;
+  const float2* table = nullptr;     // NULL: not turned
+  int64_t table_stride = 0;
+  int32_t batch = 0, n_new = 0, n_q_heads = 0, n_kv_heads = 0, max_base = 0, offset = 0, rope_dim = 0;
+  int32_t tokens = 1;                // of a workgroup
+  float eps = 0.f, rope_scale = 1.f;
+  bool pairs_order = false;
+};
+hipError_t launch_qk_norm(pic_dtype dt, int head_dim, bool interleaved, int n_layers, QkNormArgs a, hipStream_t stream);
+
+// Page tables grown on the device (every array there): room for slots [len, len + n) of request b, len = base_len[b] +
+// offset, n = page_new_tokens(b).  workspace: page_grow_workspace(...) bytes.
+struct PageGrowArgs {
+  int32_t* refs = nullptr;         // [n_pages]
+  int32_t* page_table = nullptr;   // [batch][table_cap]
+  const int32_t* base_len = nullptr;
+  const int32_t* n_valid = nullptr;
+  int32_t* pairs = nullptr;        // [batch][2]
+  int32_t* ready = nullptr;        // [batch]
+  int32_t* result = nullptr;       // [3]
+  int32_t* workspace = nullptr;
+  int32_t n_pages = 0, table_cap = 0, shift = 0, batch = 0, n_new = 0, offset = 0;
+};
+// Table entries a call looks at, at most.
+inline int64_t page_grow_entries(int32_t page_tokens, int32_t table_cap, int32_t batch, int32_t n_new) {
+  return n_new <= 0 ? 0 : (int64_t)batch * std::min<int64_t>((int64_t)(n_new - 1) / page_tokens + 2, table_cap);
+}
+hipError_t launch_page_grow(const PageGrowArgs& a, hipStream_t stream);
+
+// Page pairs[i][1] = page pairs[i][0] for the `cap` pairs on the device; those outside [0, n_pages) are none.
+hipError_t launch_page_copy_listed(void* pages_k, void* pages_v, int64_t n_streams, int64_t n_pages, int64_t page_bytes,
+                                   const int32_t* pairs, int32_t cap, hipStream_t stream);
 
 }  // namespace pic

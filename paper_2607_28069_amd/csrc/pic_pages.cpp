@@ -11,14 +11,7 @@
 #include "pic_check.h"
 #include "pic_internal.h"
 
-using namespace pic;
-
-namespace {
-
-// Slots of a request that attention reads: positions rounded up to a workgroup's tile stay in 31 bits.
-constexpr int64_t kMaxSlots = int64_t(1) << 30;
-
-int page_shift(int32_t page_tokens) { return __builtin_ctz((unsigned)page_tokens); }
+namespace pic {
 
 pic_status check_pages(const pic_pages* pg) {
   if (pg == nullptr) return fail(PIC_ERR_INVALID_ARG, "pages is NULL");
@@ -30,6 +23,17 @@ pic_status check_pages(const pic_pages* pg) {
     return fail(PIC_ERR_UNSUPPORTED, "%d pages of %d tokens: more than INT32_MAX rows", pg->n_pages, p);
   return PIC_OK;
 }
+
+}  // namespace pic
+
+using namespace pic;
+
+namespace {
+
+// Slots of a request that attention reads: positions rounded up to a workgroup's tile stay in 31 bits.
+constexpr int64_t kMaxSlots = int64_t(1) << 30;
+
+int page_shift(int32_t page_tokens) { return __builtin_ctz((unsigned)page_tokens); }
 
 // Host arrays of the bookkeeping calls.
 pic_status check_table(const pic_pages* pg, int32_t batch, const void* refs, const void* page_table) {

@@ -1,0 +1,163 @@
+// C ABI of libpic, attention of new tokens over pages for batches that share prefixes: checks, launch planning, dispatch.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "pic.h"
+#include "pic_check.h"
+#include "pic_internal.h"
+
+namespace pic {
+
+// Key ranges of a launch: the tiles of 64 keys that all workgroups take together, shared out evenly over two workgroups
+// per compute unit, of 4 tiles at least.
+SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, int32_t max_ctx) {
+  SharedPlan p;
+  const int64_t n_rep = s.n_q_heads / s.n_kv_heads;
+  const int64_t own_rows = n_new * n_rep, group_rows = m.max_group * own_rows;
+  p.row_blocks = group_rows > 64 ? 2 : 1;
+  const int64_t rows = 64 * p.row_blocks;
+  p.prefix_row_tiles = (int32_t)((group_rows + rows - 1) / rows);
+  p.own_row_tiles = (int32_t)((own_rows + rows - 1) / rows);
+  const int32_t prefix_tiles = std::min(m.max_len, max_ctx) / kSharedKeys;
+  const int32_t own_tiles = (int32_t)(((int64_t)max_ctx + n_new - prefix_tiles * kSharedKeys + kSharedKeys - 1) / kSharedKeys);
+  const int64_t heads = (int64_t)s.n_kv_heads * s.n_layers;
+  const int64_t prefix_units = m.n_groups * heads * p.prefix_row_tiles, own_units = s.batch * heads * p.own_row_tiles;
+  const int64_t per = std::max<int64_t>(4, (prefix_units * prefix_tiles + own_units * own_tiles + 511) / 512);
+  auto splits = [&](int64_t tiles) { return (int32_t)std::min<int64_t>(64, (tiles + per - 1) / per); };
+  p.prefix_splits = splits(prefix_tiles);
+  p.own_splits = splits(own_tiles);
+  p.prefix_blocks = prefix_units / s.n_layers * p.prefix_splits;
+  p.own_blocks = own_units / s.n_layers * p.own_splits;
+  p.ws_bytes = (size_t)s.n_layers * s.batch * n_new * s.n_q_heads * (p.prefix_splits + p.own_splits) * (s.head_dim + 2) * sizeof(float);
+  return p;
+}
+
+}  // namespace pic
+
+using namespace pic;
+
+namespace {
+
+// Slots of a request that attention reads: positions rounded up to a workgroup's tile stay in 31 bits.
+constexpr int64_t kMaxSlots = int64_t(1) << 30;
+
+pic_status check_shared(const pic_shared* sh) {
+  if (sh == nullptr) return fail(PIC_ERR_INVALID_ARG, "shared is NULL");
+  if (sh->n_groups < 1 || sh->max_group < 0 || sh->max_len < 0)
+    return fail(PIC_ERR_INVALID_ARG, "n_groups < 1, or max_group or max_len < 0");
+  return PIC_OK;
+}
+
+// The sizes of a call whose new tokens come after `max_ctx` slots at most, and its plan.
+pic_status check_sizes(const pic_model* m, const pic_shared* sh, int32_t batch, int32_t n_new, int64_t max_ctx, SharedMap* groups,
+                       SharedPlan* plan) {
+  if (batch < 0 || n_new < 0 || max_ctx < 0) return fail(PIC_ERR_INVALID_ARG, "negative size");
+  if (max_ctx + n_new > kMaxSlots) return fail(PIC_ERR_CAPACITY, "%lld slots per request (at most 2^30)", (long long)max_ctx + n_new);
+  if ((int64_t)batch * m->n_q_heads * n_new > INT32_MAX) return fail(PIC_ERR_UNSUPPORTED, "too many query rows");
+  if ((int64_t)n_new * m->n_kv_heads >= (int64_t(1) << 24)) return fail(PIC_ERR_UNSUPPORTED, "too many new tokens per request");
+  if (m->n_layers > 65535) return fail(PIC_ERR_UNSUPPORTED, "more than 65535 layers");
+  groups->n_groups = sh->n_groups;
+  groups->max_group = std::min(sh->max_group, batch);
+  groups->max_len = sh->max_len;
+  groups->batch = batch;
+  if (batch == 0 || n_new == 0 || m->n_layers == 0 || m->dtype != PIC_BF16) return PIC_OK;
+  *plan = plan_shared(shape_of(m, batch, 0, 0.f), *groups, n_new, (int32_t)max_ctx);
+  if (plan->prefix_blocks + plan->own_blocks >= (int64_t(1) << 24)) return fail(PIC_ERR_UNSUPPORTED, "too many workgroups");
+  return PIC_OK;
+}
+
+pic_status shared_attn(const pic_model* model, const pic_pages* pages, const pic_shared* shared, const void* q, const void* k_new,
+                       const void* v_new, void* pages_k, void* pages_v, const int32_t* page_table, int32_t batch,
+                       const int32_t* group_start, const int32_t* shared_len, const int32_t* base_len, int32_t max_base,
+                       int32_t offset, const int32_t* n_valid, int32_t n_new, float scale, bool decode, void* out, void* workspace,
+                       size_t ws_bytes, void* stream) {
+  PIC_CHECK(check_model(model));
+  PIC_CHECK(check_pages(pages));
+  PIC_CHECK(check_shared(shared));
+  if (max_base < 0 || offset < 0) return fail(PIC_ERR_INVALID_ARG, "negative size");
+  if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(PIC_ERR_INVALID_ARG, "scale must be finite and >= 0");
+  SharedMap groups;
+  SharedPlan plan;
+  PIC_CHECK(check_sizes(model, shared, batch, n_new, (int64_t)max_base + offset, &groups, &plan));
+  const int64_t max_len = (int64_t)max_base + offset + n_new;
+  if (std::max<int64_t>(max_len, shared->max_len) > (int64_t)pages->table_cap * pages->page_tokens)
+    return fail(PIC_ERR_CAPACITY, "%lld slots per request exceed a page table of %d pages of %d tokens",
+                (long long)std::max<int64_t>(max_len, shared->max_len), pages->table_cap, pages->page_tokens);
+  if (batch == 0 || n_new == 0 || model->n_layers == 0) return ok();
+  if (pages->n_pages == 0) return fail(PIC_ERR_RANGE, "no pages");
+  PIC_CHECK(check_ptr(q, "q"));
+  PIC_CHECK(check_ptr(k_new, decode ? "k_new" : "k_suf"));
+  PIC_CHECK(check_ptr(v_new, decode ? "v_new" : "v_suf"));
+  PIC_CHECK(check_ptr(pages_k, "pages_k"));
+  PIC_CHECK(check_ptr(pages_v, "pages_v"));
+  PIC_CHECK(check_ptr(out, "out"));
+  if (!page_table) return fail(PIC_ERR_INVALID_ARG, "page_table is NULL");
+  if (!base_len) return fail(PIC_ERR_INVALID_ARG, decode ? "base_len is NULL" : "ctx_len is NULL");
+  if (!shared_len) return fail(PIC_ERR_INVALID_ARG, "shared_len is NULL");
+  if (!group_start && shared->n_groups != 1) return fail(PIC_ERR_INVALID_ARG, "group_start is NULL, and there are %d groups", shared->n_groups);
+  if (model->dtype == PIC_F32) {   // (bound by the float32 matrix rate, whatever is read)
+    return decode ? pic_page_decode_attn(model, pages, q, k_new, v_new, pages_k, pages_v, page_table, batch, base_len, offset, max_base,
+                                         scale, 0, out, workspace, ws_bytes, stream)
+                  : pic_page_suffix_attn(model, pages, q, k_new, v_new, pages_k, pages_v, page_table, batch, base_len, max_base,
+                                         n_valid, n_new, scale, out, workspace, ws_bytes, stream);
+  }
+  if (!workspace || ws_bytes < plan.ws_bytes)
+    return fail(PIC_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", plan.ws_bytes, workspace ? ws_bytes : (size_t)0);
+  PIC_CHECK(check_ptr(workspace, "workspace"));
+  groups.start = group_start;
+  groups.len = shared_len;
+  PageAttnArgs a;
+  a.s = shape_of(model, batch, pages->n_pages * pages->page_tokens, scale);
+  a.map.table = page_table;
+  a.map.cap = pages->table_cap;
+  a.map.n_pages = pages->n_pages;
+  a.map.shift = __builtin_ctz((unsigned)pages->page_tokens);
+  a.q = q;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.pages_k = pages_k;
+  a.pages_v = pages_v;
+  a.base_len = base_len;
+  a.n_valid = n_valid;
+  a.max_base = max_base;
+  a.offset = offset;
+  a.n_new = n_new;
+  a.out = out;
+  a.workspace = workspace;
+  a.ws_bytes = plan.ws_bytes;
+  a.stream = (hipStream_t)stream;
+  return hip_status(launch_shared_bf16_pages(a, groups, plan), decode ? "shared decode launch" : "shared suffix launch");
+}
+
+}  // namespace
+
+PIC_API size_t pic_page_shared_workspace_bytes(const pic_model* model, const pic_shared* shared, int32_t batch, int32_t n_new,
+                                               int32_t max_ctx) {
+  SharedMap groups;
+  SharedPlan plan;
+  if (check_model(model) != PIC_OK || check_shared(shared) != PIC_OK) return 0;
+  if (check_sizes(model, shared, batch, n_new, max_ctx, &groups, &plan) != PIC_OK) return 0;
+  return plan.ws_bytes;
+}
+
+PIC_API pic_status pic_page_shared_suffix_attn(const pic_model* model, const pic_pages* pages, const pic_shared* shared, const void* q,
+                                               const void* k_suf, const void* v_suf, void* pages_k, void* pages_v,
+                                               const int32_t* page_table, int32_t batch, const int32_t* group_start,
+                                               const int32_t* shared_len, const int32_t* ctx_len, int32_t max_ctx,
+                                               const int32_t* n_valid, int32_t n_suffix, float scale, void* out, void* workspace,
+                                               size_t ws_bytes, void* stream) {
+  return shared_attn(model, pages, shared, q, k_suf, v_suf, pages_k, pages_v, page_table, batch, group_start, shared_len, ctx_len,
+                     max_ctx, 0, n_valid, n_suffix, scale, false, out, workspace, ws_bytes, stream);
+}
+
+PIC_API pic_status pic_page_shared_decode_attn(const pic_model* model, const pic_pages* pages, const pic_shared* shared, const void* q,
+                                               const void* k_new, const void* v_new, void* pages_k, void* pages_v,
+                                               const int32_t* page_table, int32_t batch, const int32_t* group_start,
+                                               const int32_t* shared_len, const int32_t* base_len, int32_t step,
+                                               int32_t max_base_len, float scale, void* out, void* workspace, size_t ws_bytes,
+                                               void* stream) {
+  return shared_attn(model, pages, shared, q, k_new, v_new, pages_k, pages_v, page_table, batch, group_start, shared_len, base_len,
+                     max_base_len, step, nullptr, 1, scale, true, out, workspace, ws_bytes, stream);
+}
