@@ -263,10 +263,12 @@ hipError_t launch_decode_bf16(const AttnShape& s, const bf16_t* q, const bf16_t*
 // Attention of n_new new tokens per request over pages (see PageAttnArgs: base_len, n_valid, max_base, offset), where
 // groups of requests share a prefix.  bf16.  The plan: `row_blocks` blocks of 64 query rows per workgroup, key ranges of
 // a group's prefix and of a request's own slots, each with that many tiles of query rows.
+constexpr int kSharedMaxSplits = 64;   // key ranges of a prefix, and of a request's own slots
 struct SharedPlan {
   int32_t row_blocks = 1, prefix_splits = 1, own_splits = 1, prefix_row_tiles = 0, own_row_tiles = 0;
   int64_t prefix_blocks = 0, own_blocks = 0;   // workgroups per layer
   size_t ws_bytes = 0;
+  bool stream = false;   // rows are read once and past the last-level cache
 };
 SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, int32_t max_ctx);
 hipError_t launch_shared_bf16_pages(const PageAttnArgs& a, const SharedMap& m, const SharedPlan& plan);

@@ -10,27 +10,82 @@
 
 namespace pic {
 
-// Key ranges of a launch: the tiles of 64 keys that all workgroups take together, shared out evenly over two workgroups
-// per compute unit, of 4 tiles at least.
+namespace {
+
+// The time of a launch, in tiles of 64 keys of a workgroup that has a compute unit to itself (about 1.2 us).  512 workgroups
+// run at once, the prefixes' before the requests' own; two on a compute unit slow each other down, and a workgroup's
+// start (lengths, page numbers, first tile) costs about 3 tiles.
+struct LaunchCost {
+  int64_t prefix_units, own_units;   // workgroups per key range
+  double both, join;                 // a tile where compute units hold two; a part's share of the combine
+
+  double operator()(int64_t prefix_tiles, int64_t prefix_splits, int64_t own_tiles, int64_t own_splits) const {
+    constexpr double kStart = 3.0;
+    const int64_t P = prefix_units * prefix_splits, O = own_units * own_splits;
+    const int64_t rest = P % 512;
+    double t = (double)prefix_tiles * ((double)(P / 512) * both + (rest == 0 ? 0.0 : rest <= 256 ? 1.0 : both)) + kStart * (double)((P + 511) / 512);
+    const double own = (double)own_tiles + kStart;
+    const int64_t beside = P < 512 ? 512 - P : 0;
+    if (O <= beside) t = std::max(t, own);
+    else t += own * (double)((std::max<int64_t>(0, O - beside * (int64_t)(t / own)) + 511) / 512);
+    return t + join * (double)(prefix_splits + own_splits);
+  }
+};
+
+int64_t ceil_of(int64_t n, int64_t d) { return (n + d - 1) / d; }
+
+}  // namespace
+
+// Key ranges of a launch: as many as cover the compute units once, one and a half times, or twice, whichever the estimate
+// above puts first, requests' own ranges filling what is left.  Measured, us by ranges of the prefix (head_dim 128, 8 kv heads):
+// 64 requests over 16K + 300 own (16 workgroups a range) 16: 41.5, 24: 47, 32: 49; 16 over 10K (8) 20: 21.3, 28: 19.0, 40:
+// 22.1; 16 x 24 tokens over 10K (96) 2: 143, 4: 92, 5: 86, 8: 107; 4 groups of up to 32K (16) 16: 63, 24: 60, 28: 57.
 SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, int32_t max_ctx) {
   SharedPlan p;
   const int64_t n_rep = s.n_q_heads / s.n_kv_heads;
   const int64_t own_rows = n_new * n_rep, group_rows = m.max_group * own_rows;
   p.row_blocks = group_rows > 64 ? 2 : 1;
-  const int64_t rows = 64 * p.row_blocks;
-  p.prefix_row_tiles = (int32_t)((group_rows + rows - 1) / rows);
-  p.own_row_tiles = (int32_t)((own_rows + rows - 1) / rows);
-  const int32_t prefix_tiles = std::min(m.max_len, max_ctx) / kSharedKeys;
-  const int32_t own_tiles = (int32_t)(((int64_t)max_ctx + n_new - prefix_tiles * kSharedKeys + kSharedKeys - 1) / kSharedKeys);
+  p.prefix_row_tiles = (int32_t)ceil_of(group_rows, 64 * p.row_blocks);
+  p.own_row_tiles = (int32_t)ceil_of(own_rows, 64);
+  const int64_t prefix_tiles = std::min(m.max_len, max_ctx) / kSharedKeys;
+  const int64_t own_tiles = ceil_of((int64_t)max_ctx + n_new - prefix_tiles * kSharedKeys, kSharedKeys);
   const int64_t heads = (int64_t)s.n_kv_heads * s.n_layers;
   const int64_t prefix_units = m.n_groups * heads * p.prefix_row_tiles, own_units = s.batch * heads * p.own_row_tiles;
-  const int64_t per = std::max<int64_t>(4, (prefix_units * prefix_tiles + own_units * own_tiles + 511) / 512);
-  auto splits = [&](int64_t tiles) { return (int32_t)std::min<int64_t>(64, (tiles + per - 1) / per); };
-  p.prefix_splits = splits(prefix_tiles);
-  p.own_splits = splits(own_tiles);
-  p.prefix_blocks = prefix_units / s.n_layers * p.prefix_splits;
-  p.own_blocks = own_units / s.n_layers * p.own_splits;
-  p.ws_bytes = (size_t)s.n_layers * s.batch * n_new * s.n_q_heads * (p.prefix_splits + p.own_splits) * (s.head_dim + 2) * sizeof(float);
+  const int64_t rows = (int64_t)s.n_layers * s.batch * n_new * s.n_q_heads, part_bytes = rows * (s.head_dim + 2) * (int64_t)sizeof(float);
+  // (groups are rarely of one size: of the row tiles that the grid has room for, about as many as the batch fills)
+  const int64_t row_tiles = std::min<int64_t>((int64_t)m.n_groups * p.prefix_row_tiles,
+                                              s.batch * own_rows / (64 * p.row_blocks) + m.n_groups);
+  LaunchCost cost;
+  cost.prefix_units = heads * row_tiles;
+  cost.own_units = own_units;
+  // (bound by the loads, which one workgroup with tiles of half the size does not keep busy, or by products)
+  cost.both = p.row_blocks == 2 ? 1.7 : s.head_dim == 64 ? 1.3 : 2.0;
+  cost.join = (double)part_bytes * 2.0 / 4.8e6;
+  double best = 1e30;
+  for (const int64_t fill : {256, 384, 512}) {
+    if (fill == 256 && m.n_groups > 1) continue;   // (nor of one length: longer ones need company)
+    int64_t n = 0, tiles = 0;
+    if (prefix_tiles > 0 && prefix_units > 0) {
+      n = std::min({std::max<int64_t>(1, fill / cost.prefix_units), prefix_tiles, (int64_t)kSharedMaxSplits});
+      tiles = ceil_of(prefix_tiles, n);
+      n = ceil_of(prefix_tiles, tiles);
+    }
+    const int64_t left = 512 - std::min<int64_t>(512, cost.prefix_units * n);
+    const int64_t o = std::max<int64_t>(1, std::min({left / own_units, (own_tiles + 1) / 2, (int64_t)kSharedMaxSplits}));
+    const double c = cost(tiles, n, ceil_of(own_tiles, o), o);
+    if (c < best) {
+      best = c;
+      p.prefix_splits = (int32_t)n;
+      p.own_splits = (int32_t)o;
+    }
+  }
+  auto blocks = [](int64_t ranges, int64_t row_tiles) { return ceil_of(ranges, 8) * 8 * row_tiles; };   // (whole rounds of the XCDs)
+  p.prefix_blocks = blocks((int64_t)m.n_groups * s.n_kv_heads * p.prefix_splits, p.prefix_row_tiles);
+  p.own_blocks = blocks((int64_t)s.batch * s.n_kv_heads * p.own_splits, p.own_row_tiles);
+  // Rows that the last-level cache (256 MB) will not hold until the next call leave it to others (8 requests x 33K in 4
+  // groups 60 -> 55 us, 64 requests of up to 2K of their own 72 -> 63; below, 16 over 10K 19.5 -> 21.2).
+  p.stream = p.prefix_row_tiles <= 1 && heads * s.head_dim * 4.0 * ((double)m.n_groups * prefix_tiles + (double)s.batch * own_tiles) * kSharedKeys > 256e6;
+  p.ws_bytes = (size_t)part_bytes * (p.prefix_splits + p.own_splits);
   return p;
 }
 
@@ -55,7 +110,7 @@ pic_status check_sizes(const pic_model* m, const pic_shared* sh, int32_t batch, 
                        SharedPlan* plan) {
   if (batch < 0 || n_new < 0 || max_ctx < 0) return fail(PIC_ERR_INVALID_ARG, "negative size");
   if (max_ctx + n_new > kMaxSlots) return fail(PIC_ERR_CAPACITY, "%lld slots per request (at most 2^30)", (long long)max_ctx + n_new);
-  if ((int64_t)batch * m->n_q_heads * n_new > INT32_MAX) return fail(PIC_ERR_UNSUPPORTED, "too many query rows");
+  if ((int64_t)batch * m->n_q_heads * n_new * std::max(m->n_layers, 1) >= (int64_t(1) << 27)) return fail(PIC_ERR_UNSUPPORTED, "too many query rows");
   if ((int64_t)n_new * m->n_kv_heads >= (int64_t(1) << 24)) return fail(PIC_ERR_UNSUPPORTED, "too many new tokens per request");
   if (m->n_layers > 65535) return fail(PIC_ERR_UNSUPPORTED, "more than 65535 layers");
   groups->n_groups = sh->n_groups;

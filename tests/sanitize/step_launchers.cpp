@@ -30,16 +30,19 @@ void wr(void* base, int64_t at, int64_t bytes) {
 hipError_t launch_shared_bf16_pages(const PageAttnArgs& a, const SharedMap& m, const SharedPlan& plan) {
   ++emu::launches;
   const AttnShape& s = a.s;
-  const int n_rep = s.n_q_heads / s.n_kv_heads, parts = plan.prefix_splits + plan.own_splits, ROWS = 64 * plan.row_blocks;
+  const int n_rep = s.n_q_heads / s.n_kv_heads, parts = plan.prefix_splits + plan.own_splits;
   const int64_t rb = (int64_t)s.head_dim * 2;
   float* ws_ml = static_cast<float*>(a.workspace) + (size_t)s.n_layers * s.batch * a.n_new * s.n_q_heads * parts * s.head_dim;
   for (int l = 0; l < s.n_layers; ++l)
     for (int64_t block = 0; block < plan.prefix_blocks + plan.own_blocks; ++block) {
       const bool prefix = block < plan.prefix_blocks;
-      int64_t at = prefix ? block : block - plan.prefix_blocks;
+      const int64_t at = prefix ? block : block - plan.prefix_blocks;
+      const int ROWS = prefix ? 64 * plan.row_blocks : 64;
       const int row_tiles = prefix ? plan.prefix_row_tiles : plan.own_row_tiles, splits = prefix ? plan.prefix_splits : plan.own_splits;
-      const int rt = at % row_tiles, split = at / row_tiles % splits, g = at / row_tiles / splits % s.n_kv_heads;
-      const int owner = (int)(at / row_tiles / splits / s.n_kv_heads), row0 = rt * ROWS;
+      const int rt = at / 8 % row_tiles;
+      const int64_t range = at / 8 / row_tiles * 8 + at % 8;
+      const int split = range % splits, g = range / splits % s.n_kv_heads, owner = (int)(range / splits / s.n_kv_heads), row0 = rt * ROWS;
+      if (owner >= (prefix ? m.n_groups : s.batch)) continue;
       int b0 = owner, n_rows, k0, k1, ctx = INT32_MAX, n_tok = 0, gi = owner;
       if (prefix) {
         b0 = m.first(owner);
@@ -59,7 +62,6 @@ hipError_t launch_shared_bf16_pages(const PageAttnArgs& a, const SharedMap& m, c
         k0 = from + std::min(split * per, tiles) * kSharedKeys;
         k1 = std::min(from + std::min(split * per + per, tiles) * kSharedKeys, end);
       }
-      int seen = 0;
       for (int r = row0; r < row0 + n_rows; ++r) {
         const int per_request = prefix ? a.n_new * n_rep : INT32_MAX;
         const int b = b0 + r / per_request, in_b = r % per_request, tok = in_b / n_rep;
@@ -69,7 +71,6 @@ hipError_t launch_shared_bf16_pages(const PageAttnArgs& a, const SharedMap& m, c
         else if (tok >= page_new_tokens(a.base_len, a.n_valid, b, a.n_new)) lim = -1;
         else lim = std::min(k1, shared_part(k1, clamp_len(a.base_len[b], a.max_base) + a.offset));
         if (lim < 0) continue;
-        seen = std::max(seen, lim);
         rd(a.q, row * rb, rb);
         const int first = prefix ? split : gi < 0 && split == 0 ? 0 : plan.prefix_splits + split;
         for (int p = first; p <= (prefix ? split : plan.prefix_splits + split); ++p) {
@@ -77,7 +78,7 @@ hipError_t launch_shared_bf16_pages(const PageAttnArgs& a, const SharedMap& m, c
           wr(ws_ml, (row * parts + p) * 8, 8);
         }
       }
-      const int k_end = std::min(k1, seen), tab = std::min(b0, s.batch - 1);
+      const int k_end = prefix ? k1 : std::min(k1, ctx + (row0 + n_rows - 1) / n_rep + 1), tab = std::min(b0, s.batch - 1);
       const int64_t stream0 = ((int64_t)l * s.n_kv_heads + g) * s.cache_cap;
       for (int wave = 0; wave < 4; ++wave) {
         const int win = std::min(k0 + 16 * wave, std::max(k_end - 1, 0) & ~15) >> a.map.shift;

@@ -11,6 +11,13 @@ from shared_path import batch, decode, starts, suffix, workspace
 
 pytestmark = pytest.mark.gpu
 
+
+def right(x, **kw):
+    """Probabilities over shared slots keep 16 bits up to 64 query rows of a group, and 8 beyond (one rounding of 2^-8 each, which
+    the numerator and the denominator see: as in a prefill)."""
+    check(x, decoded=x.shared.max_group * x.n * (x.hq // x.hkv) <= 64, **kw)
+
+
 HEADS = [(4, 2, 64), (32, 8, 128), (28, 4, 128), (5, 1, 64), (3, 3, 128), (40, 1, 128)]
 
 
@@ -21,7 +28,7 @@ def test_decode(hq, hkv, d, P):
     ctx = [333, 400, 333, 511, 70, 20, 0, 190, -1, 130]
     x = batch(hq, hkv, d, P, ctx, [1] * 10, [0, 4, 5, 7, 10], [333, 70, 0, 130])
     decode(x)
-    check(x, decoded=True)
+    right(x)
 
 
 @pytest.mark.parametrize("shared", [1, 15, 63, 64, 65, 127, 128, 200])
@@ -30,7 +37,7 @@ def test_decode_borders(shared, own):
     for P in (16, 128):
         x = batch(8, 2, 128, P, [shared + own, shared, shared + own // 2], [1] * 3, [0, 3], [shared], slack=9)
         decode(x)
-        check(x, decoded=True)
+        right(x)
 
 
 @pytest.mark.parametrize("sizes", [[2], [17], [33], [1, 40, 3], [16, 16, 16, 16]])
@@ -42,7 +49,7 @@ def test_decode_groups(sizes, hq, hkv, d):
     ctx = [s + int(r.integers(0, 150)) for s, n in zip(shared, sizes) for _ in range(n)]
     x = batch(hq, hkv, d, 32, ctx, [1] * len(ctx), starts(sizes), shared, L=2)
     decode(x, step=3)
-    check(x, decoded=True)
+    right(x)
 
 
 @pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (28, 4, 128), (4, 2, 64), (40, 1, 64)])
@@ -52,26 +59,26 @@ def test_suffix(hq, hkv, d, n):
     new = [n, 1, n // 2, 0, n, n - 1, n, n]
     x = batch(hq, hkv, d, 64, ctx, new, [0, 4, 5, 8], [640, 0, 90], n=n)
     suffix(x)
-    check(x, decoded=True)
+    right(x)
 
 
 @pytest.mark.parametrize("n", [1, 33])
 def test_suffix_row_tiles(n):
     x = batch(32, 4, 128, 16, [1300, 1290, 1300, 1281, 1300, 1500], [n] * 6, [0, 6], [1281], n=n, L=2)
     suffix(x, n_valid=None)
-    check(x, decoded=True)
+    right(x)
 
 
 def test_no_groups_and_all_in_one():
     """Without starts the batch is one group; requests before the first start and after the last share nothing."""
     x = batch(8, 2, 128, 64, [200, 210, 250], [1] * 3, [0, 3], [200])
     decode(x, start=None)
-    check(x, decoded=True)
+    right(x)
     x = batch(8, 2, 128, 64, [200, 210, 250, 300, 100], [1] * 5, [0, 1, 4, 5], [0, 200, 0])
     x.start, x.shared_len = x.start[1:3].clone(), x.shared_len[1:2].clone()
     x.shared = pic.Shared.of(1, 3, 200)
     decode(x)
-    check(x, decoded=True)
+    right(x)
 
 
 def test_bounds_below_the_lengths():
@@ -79,17 +86,17 @@ def test_bounds_below_the_lengths():
     x = batch(8, 2, 128, 64, [400, 410, 450, 401], [1] * 4, [0, 4], [400])
     x.shared = pic.Shared.of(1, 2, 300)
     decode(x)
-    check(x, decoded=True)
+    right(x)
 
 
 def test_requests_shorter_than_the_prefix():
     """Requests whose new tokens come before the end of the shared slots see their own slots only."""
     x = batch(8, 2, 128, 32, [500, 100, 63, 64, 0, 430], [1] * 6, [0, 6], [480])
     decode(x)
-    check(x, decoded=True)
+    right(x)
     x = batch(8, 2, 64, 32, [500, 100, 63, 64, 0, 430], [9] * 6, [0, 6], [480], n=9)
     suffix(x)
-    check(x, decoded=True)
+    right(x)
 
 
 def test_prefix_held_by_padding():
@@ -99,14 +106,14 @@ def test_prefix_held_by_padding():
     x.K[0], x.V[0] = x.K[0][:, :, :330], x.V[0][:, :, :330]
     x.len[0] = -1
     decode(x)
-    check(x, decoded=True)
+    right(x)
 
 
 def test_a_batch_of_padding():
     x = batch(8, 2, 128, 64, [-1, -1], [1, 1], [0, 2], [0])
     x.shared_len[0] = 64
     decode(x)
-    check(x, decoded=True)
+    right(x)
 
 
 def test_the_same_bits_twice_and_with_a_larger_workspace():
@@ -125,7 +132,7 @@ def test_the_same_bits_twice_and_with_a_larger_workspace():
 def test_scale():
     x = batch(8, 2, 128, 64, [300, 350], [1] * 2, [0, 2], [300])
     decode(x, scale=0.03)
-    check(x, scale=0.03, decoded=True)
+    right(x, scale=0.03)
 
 
 @pytest.mark.parametrize("n", [1, 3])
@@ -150,7 +157,7 @@ def test_rows_past_2_32_bytes():
     x.table = torch.from_numpy(x.table_host).to(DEV)
     x.pages = pic.Pages.of(n_pages, P, x.pages.table_cap)
     decode(x)
-    check(x, decoded=True)
+    right(x)
 
 
 def _odd(x, kind):
@@ -199,7 +206,7 @@ def test_values_that_are_not_finite(n, kind):
         x.V[b] = torch.where(torch.isfinite(x.V[b]), x.V[b], torch.zeros_like(x.V[b]))
     ref, mag, _ = reference(x)
     ok = torch.isfinite(got)
-    assert ((got.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -14 * mag + 1e-30)[ok].all()
+    assert ((got.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** (-14 if 3 * n * 8 <= 64 else -7) * mag + 1e-30)[ok].all()   # (see right())
 
 
 def test_keys_that_are_not_finite():
@@ -238,7 +245,7 @@ def test_streams_and_graph():
     x = batch(32, 8, 128, 64, [900, 910, 950, 980], [1] * 4, [0, 4], [900], slack=64)
     ws = workspace(x, 1, x.max_ctx)
     eager = decode(x, ws=ws).clone()
-    check(x, decoded=True)
+    right(x)
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
         decode(x, ws=ws)
@@ -268,7 +275,7 @@ def test_streams_and_graph():
         decode(x, ws=torch.empty_like(ws))
     torch.cuda.synchronize()
     assert (x.out == replayed).all()
-    check(x, decoded=True)
+    right(x)
 
 
 def test_bad_tables_stay_in_bounds():
