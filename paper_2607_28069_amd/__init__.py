@@ -652,31 +652,28 @@ def pic_page_copy_async(model: Model, pages: Pages, pages_k, pages_v, pairs, pai
     _check(load().pic_page_copy_async(ctypes.byref(model), ctypes.byref(pages), k, v, pr, int(pair_cap), st))
 
 
-def _token_rows(t, heads, head_dim, name):
-    """(address, elements from token to token) of rows [..., heads, head_dim] on the current device, dense within a token
-    and one step from token to token: a dense tensor or a slice of a wider row."""
+def _token_rows(t, heads, head_dim, name, at):
+    """(address, elements from token to token) of rows [..., heads, head_dim] on device `at`, dense within a token and one
+    step from token to token: a dense tensor or a slice of a wider row."""
     if t is None:
         return None, 0
-    if t.dim() < 2 or t.shape[-1] != head_dim or t.shape[-2] != heads:
-        raise ValueError(f"{name}: [..., {heads}, {head_dim}] expected, got {tuple(t.shape)}")
-    step = heads * head_dim
-    if not t.is_contiguous():
-        if t.stride(-1) != 1 or (heads > 1 and t.stride(-2) != head_dim):
-            raise ValueError(f"{name}: a token's heads must be dense")
-        span = None   # of the token dimensions met so far, innermost first
-        for size, stride in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):
-            if size == 1:
-                continue
-            if span is None:
-                step = stride
-            elif stride != span:
-                raise ValueError(f"{name}: tokens must lie one step apart")
-            span = size * stride
-    if not t.is_cuda:
-        raise ValueError("device buffer expected: got a host tensor")
-    import torch
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} on device {t.get_device()}, the current one is {torch.cuda.current_device()}")
+    shape, strides = t.shape, t.stride()
+    if len(shape) < 2 or shape[-1] != head_dim or shape[-2] != heads:
+        raise ValueError(f"{name}: [..., {heads}, {head_dim}] expected, got {tuple(shape)}")
+    if strides[-1] != 1 or (strides[-2] != head_dim and heads > 1):
+        raise ValueError(f"{name}: a token's heads must be dense")
+    step, span = 0, None   # span: of the token dimensions met so far, innermost first
+    for i in range(len(shape) - 3, -1, -1):
+        if shape[i] == 1:
+            continue
+        if span is None:
+            step = strides[i]
+        elif strides[i] != span:
+            raise ValueError(f"{name}: tokens must lie one step apart")
+        span = shape[i] * strides[i]
+    if t.get_device() != at:   # (-1 for a host tensor)
+        raise ValueError("device buffer expected: got a host tensor" if not t.is_cuda else
+                         f"{name} on device {t.get_device()}, the current one is {at}")
     return t.data_ptr(), step
 
 
@@ -685,9 +682,11 @@ def pic_qk_norm_rope(model: Model, how: QkNorm, q, k, v, batch, n_new, table, ma
     """q [..., n_q_heads, D], k and v [..., n_kv_heads, D] (tokens dense or a step apart; None: left out) to dense q_out, k_out,
     v_out: heads normalised and turned to positions base_len[b] + offset + i."""
     hq, hkv, d = model.n_q_heads, model.n_kv_heads, model.head_dim
+    import torch
+    at = torch.cuda.current_device()
     (lens, nv, tab, qo, ko, vo), st = _on_device((base_len, n_valid, table, q_out, k_out, v_out), stream)
-    _check(load().pic_qk_norm_rope(ctypes.byref(model), ctypes.byref(how), *_token_rows(q, hq, d, "q"),
-                                   *_token_rows(k, hkv, d, "k"), *_token_rows(v, hkv, d, "v"), int(batch), lens,
+    _check(load().pic_qk_norm_rope(ctypes.byref(model), ctypes.byref(how), *_token_rows(q, hq, d, "q", at),
+                                   *_token_rows(k, hkv, d, "k", at), *_token_rows(v, hkv, d, "v", at), int(batch), lens,
                                    int(max_base_len), int(offset), nv, int(n_new), tab, int(max_abs_delta), qo, ko, vo, st))
 
 

@@ -273,6 +273,7 @@ struct SharedPlan {
 SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, int32_t max_ctx);
 hipError_t launch_shared_bf16_pages(const PageAttnArgs& a, const SharedMap& m, const SharedPlan& plan);
 
+constexpr int32_t kQkNormHeads = 2;   // heads of one token that the same lanes take
 // Norms of queries and keys with their rotation (rows of a token at q + token * q_stride and so on, token = (layer *
 // batch + request) * n_new + i; dense outputs).  Positions clamp_len(base_len[b], max_base) + offset + i, or offset + i
 // without base_len, all inside the table.
@@ -291,7 +292,6 @@ struct QkNormArgs {
   const float2* table = nullptr;     // NULL: not turned
   int64_t table_stride = 0;
   int32_t batch = 0, n_new = 0, n_q_heads = 0, n_kv_heads = 0, max_base = 0, offset = 0, rope_dim = 0;
-  int32_t tokens = 1;                // of a workgroup
   float eps = 0.f, rope_scale = 1.f;
   bool pairs_order = false;
 };

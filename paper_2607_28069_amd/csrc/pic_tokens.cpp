@@ -85,13 +85,12 @@ PIC_API pic_status pic_qk_norm_rope(const pic_model* model, const pic_qk_norm* h
     PIC_CHECK(check_ptr(table, "table"));
   }
   if (model->n_layers > 65535) return fail(PIC_ERR_UNSUPPORTED, "more than 65535 layers");
-  if ((int64_t)model->n_q_heads + 2 * (int64_t)model->n_kv_heads > 65536) return fail(PIC_ERR_UNSUPPORTED, "more than 65536 heads");
   QkNormArgs a;
-  // a few tokens a workgroup: enough rows to keep its loads on their way, few enough that short calls use the GPU
-  const int64_t tokens = (int64_t)model->n_layers * batch * n_new;
-  const int32_t heads = (q ? model->n_q_heads : 0) + (k ? model->n_kv_heads : 0) + (v ? model->n_kv_heads : 0);
-  if (heads > 0) a.tokens = (int32_t)std::max<int64_t>(1, std::min<int64_t>({tokens / 2048, 256 / heads, n_new}));
-  if ((int64_t)batch * ((n_new + (int64_t)a.tokens - 1) / a.tokens) >= (int64_t(1) << 24))
+  // (items of kQkNormHeads heads of a token; a grid holds fewer than 2^32 threads)
+  const int64_t rows = (int64_t)batch * n_new, tokens = rows < (int64_t(1) << 28) ? model->n_layers * rows : rows;
+  auto chunks = [](const void* x, int64_t heads) { return x ? (heads + kQkNormHeads - 1) / kQkNormHeads : 0; };
+  const int64_t heads = chunks(q, model->n_q_heads) + chunks(k, model->n_kv_heads) + chunks(v, model->n_kv_heads);
+  if (tokens >= (int64_t(1) << 28) || heads >= (int64_t(1) << 28) || tokens * heads * 16 >= (int64_t(1) << 32))
     return fail(PIC_ERR_UNSUPPORTED, "too many tokens in one call");
   if (tokens == 0 || heads == 0) return ok();
   if (!aligned16(how->q_weight)) return fail(PIC_ERR_MISALIGNED, "q_weight is not 16-byte aligned");

@@ -113,21 +113,20 @@ hipError_t launch_shared_bf16_pages(const PageAttnArgs& a, const SharedMap& m, c
 hipError_t launch_qk_norm(pic_dtype dt, int head_dim, bool, int n_layers, QkNormArgs a, hipStream_t) {
   ++emu::launches;
   const int64_t es = dt == PIC_F32 ? 4 : 2, rb = head_dim * es;
-  const int per = (a.n_new + a.tokens - 1) / a.tokens;
   for (int l = 0; l < n_layers; ++l)
-    for (int64_t block = 0; block < (int64_t)per * a.batch; ++block) {
-      const int b = (int)(block / per), i0 = (int)(block % per) * a.tokens;
-      int n_tok = a.n_new;
-      int64_t pos0 = a.offset;
-      if (a.base_len) {
-        n_tok = page_new_tokens(a.base_len, a.n_valid, b, a.n_new);
-        pos0 += clamp_len(a.base_len[b], a.max_base);
-      } else if (a.n_valid) {
-        n_tok = clamp_len(a.n_valid[b], a.n_new);
-      }
-      for (int t = 0; t < std::min(n_tok - i0, a.tokens); ++t) {
-        const int64_t tok = ((int64_t)l * a.batch + b) * a.n_new + i0 + t;
-        if (a.table) rd(a.table + l * a.table_stride, (pos0 + i0 + t) * (head_dim / 2) * 8, head_dim / 2 * 8);
+    for (int b = 0; b < a.batch; ++b)
+      for (int i = 0; i < a.n_new; ++i) {
+        int n_tok = a.n_new;
+        int64_t pos = a.offset + i;
+        if (a.base_len) {
+          n_tok = page_new_tokens(a.base_len, a.n_valid, b, a.n_new);
+          pos += clamp_len(a.base_len[b], a.max_base);
+        } else if (a.n_valid) {
+          n_tok = clamp_len(a.n_valid[b], a.n_new);
+        }
+        if (i >= n_tok) continue;
+        const int64_t tok = ((int64_t)l * a.batch + b) * a.n_new + i;
+        if (a.table) rd(a.table + l * a.table_stride, pos * (head_dim / 2) * 8, head_dim / 2 * 8);
         auto rows = [&](const void* in, void* out, int64_t stride, int heads, const float* w) {
           for (int h = 0; in && h < heads; ++h) {
             rd(in, (tok * stride + (int64_t)h * head_dim) * es, rb);
@@ -139,7 +138,6 @@ hipError_t launch_qk_norm(pic_dtype dt, int head_dim, bool, int n_layers, QkNorm
         rows(a.k, a.k_out, a.k_stride, a.n_kv_heads, a.k_weight);
         rows(a.v, a.v_out, a.v_stride, a.n_kv_heads, nullptr);
       }
-    }
   return hipSuccess;
 }
 

@@ -163,9 +163,12 @@ def test_norm_binding_refusals():
     rows = pic._token_rows
     for bad in (q[..., :3, :], q[..., :32], q.transpose(0, 1), q.transpose(2, 3), torch.zeros(4, 3, 8, 128)[::2, :, :4, ::2]):
         with pytest.raises(ValueError):
-            rows(bad, 4, 64, "q")
+            rows(bad, 4, 64, "q", -1)
+    assert rows(q, 4, 64, "q", -1) == (q.data_ptr(), 256)
+    wide = torch.zeros(2, 3, 5 * 64)
+    assert rows(wide[..., 64:].unflatten(-1, (4, 64)), 4, 64, "q", -1) == (wide.data_ptr() + 256, 320)
     with pytest.raises(ValueError, match="host"):
-        rows(q, 4, 64, "q")
+        rows(q, 4, 64, "q", 0)
     assert how.eps > 0
     with pytest.raises(ValueError, match="float32"):
         pic.QkNorm.of(torch.zeros(64, dtype=torch.bfloat16), None)
