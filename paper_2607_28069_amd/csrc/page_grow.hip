@@ -2,8 +2,10 @@
 // the page copies that it asks for.
 //
 // Growing is a few integers behind a chain of loads that wait for one another (lengths -> table entries -> reference
-// counts -> free pages -> the entries that take them), so one workgroup does it all: what
-// bounds it is that chain, and a second workgroup would add a launch or a wait between the two.  The order of the host's
+// counts -> free pages -> the entries that take them), so one workgroup does it all: that chain bounds it, and a second
+// workgroup would add a launch or a wait between the two.  What can be asked for early is (the first pages' counts), and
+// what the first pass over a decode step's entries finds stays in registers: 64 requests of 16384 tokens over 20000 pages
+// of 64 7.8 us, where a pass that found each place again before every step took 10.6.  The order of the host's
 // loop (request by request, entry by entry) comes from prefix sums over the workgroup; where several entries hold the
 // same shared page, the k-th of them takes a page of its own if the page has more than k + 1 references, so the last
 // ones keep it.  Nothing is changed before it is known that everything fits.
@@ -41,36 +43,44 @@ __device__ __forceinline__ Scan scan(int x, int (&sums)[kWaves]) {
 
 // 1 workgroup.  workspace: first[batch + 1] (a request's first entry in the order), then of every entry in the order its
 // page where it is shared (shared[]), where in the order that was (at[]) and what becomes of it (take[]), and the free
-// pages in order (lowest[]).
+// pages in order (lowest[]).  The first kThreads entries, which are all of them in a decode step, stay in registers, the
+// first kFirst requests' places in LDS, and the first pages' reference counts are on their way from the start.
 __global__ void __launch_bounds__(kThreads) page_grow_kernel(PageGrowArgs a, int32_t cap_entries) {
+  constexpr int kFirst = 4096, kPer = 16;   // requests in LDS; pages a thread looks at at once
   __shared__ int sums[kWaves];
+  __shared__ int32_t first_lds[kFirst + 1];
   __shared__ int bad_cap, bad_entry;
   const int tid = threadIdx.x;
-  int32_t* first = a.workspace;
-  int32_t* shared = first + a.batch + 1;
+  int32_t* first = a.batch <= kFirst ? first_lds : a.workspace;
+  int32_t* shared = a.workspace + a.batch + 1;
   int32_t* at = shared + cap_entries;
   int32_t* take = at + cap_entries;
   int32_t* lowest = take + cap_entries;
   const int32_t P = 1 << a.shift;
+  int4 refs[kPer / 4];
+  auto look = [&](int64_t p0) {   // at pages [p0, p0 + kPer) (past the last one: not free)
+#pragma unroll
+    for (int u = 0; u < kPer / 4; ++u) {
+      const int64_t p = p0 + 4 * u;
+      if (p + 4 <= a.n_pages) __builtin_memcpy(&refs[u], a.refs + p, 16);   // (refs is 4-byte aligned)
+      else refs[u] = make_int4(p < a.n_pages ? a.refs[p] : 1, p + 1 < a.n_pages ? a.refs[p + 1] : 1, p + 2 < a.n_pages ? a.refs[p + 2] : 1, 1);
+    }
+  };
+  look((int64_t)kPer * tid);
   if (tid == 0) bad_cap = bad_entry = 0;
   __syncthreads();
-  // a request's new slots: [from, to), empty where it is left alone
-  auto slots = [&](int b, int64_t& from, int64_t& to) {
-    const int32_t base = a.base_len[b];
-    from = (int64_t)base + a.offset;
-    to = from + page_new_tokens(a.base_len, a.n_valid, b, a.n_new);
-    return to > from;
-  };
-  // 1. the entries each request's new slots lie in
+  // 1. the entries each request's new slots, [base + offset, + n), lie in
   int32_t entries = 0;
   for (int b0 = 0; b0 < a.batch; b0 += kThreads) {
     const int b = b0 + tid;
     int n = 0;
-    int64_t from, to;
-    if (b < a.batch && slots(b, from, to)) {
+    if (b < a.batch) {
+      const int64_t from = (int64_t)a.base_len[b] + a.offset, to = from + page_new_tokens(a.base_len, a.n_valid, b, a.n_new);
       const int64_t end = (to + P - 1) >> a.shift;
-      if (end > a.table_cap) bad_cap = 1;
-      else n = (int)(end - (from >> a.shift));
+      if (to > from) {
+        if (end > a.table_cap) bad_cap = 1;
+        else n = (int)(end - (from >> a.shift));
+      }
     }
     const Scan s = scan(n, sums);
     if (b < a.batch) first[b] = entries + s.before;
@@ -79,114 +89,128 @@ __global__ void __launch_bounds__(kThreads) page_grow_kernel(PageGrowArgs a, int
   if (tid == 0) first[a.batch] = entries;
   __syncthreads();
   bool fits = bad_cap == 0;   // (then at most cap_entries of them)
-  // entry e of the order: its request and place in the table
-  auto locate = [&](int e, int& b, int32_t& i, bool& partly) {
+  // Entry e of the order: where it lies in the table, and whether new slots take only part of it.
+  struct Place {
+    int32_t* entry;
+    bool partly;
+  };
+  auto locate = [&](int e) -> Place {
     int lo = 0, hi = a.batch;   // first[lo] <= e < first[hi]
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (first[mid] <= e) lo = mid;
       else hi = mid;
     }
-    b = lo;
-    const int64_t from = (int64_t)a.base_len[b] + a.offset;
-    i = (int32_t)(from >> a.shift) + (e - first[b]);
-    partly = e == first[b] && (from & (P - 1)) != 0;
+    const int64_t from = (int64_t)a.base_len[lo] + a.offset;
+    return {a.page_table + (int64_t)lo * a.table_cap + (from >> a.shift) + (e - first[lo]), e == first[lo] && (from & (P - 1)) != 0};
   };
-  // 2. what becomes of each: 0 kept, 1 takes a page, 2 shared (settled below)
-  int32_t n_shared = 0;
+  // 2. what becomes of each: 0 kept, 1 takes a page, 2 shared (settled below).  In the order, `ranks` entries take a page before
+  // this thread's of the first kThreads (where none is shared).
+  int32_t n_shared = 0, takes = 0;
+  Place place = {nullptr, false};
+  int32_t page0 = -1;
+  int kind0 = 0, ranks = 0;
   if (fits) {
     for (int e0 = 0; e0 < entries; e0 += kThreads) {
       const int e = e0 + tid;
       int kind = 0;
       int32_t page = -1;
       if (e < entries) {
-        int b;
-        int32_t i;
-        bool partly;
-        locate(e, b, i, partly);
-        page = a.page_table[(int64_t)b * a.table_cap + i];
-        if (page == -1 && !partly) {
+        const Place x = locate(e);
+        page = *x.entry;
+        if (page == -1 && !x.partly) {
           kind = 1;
         } else if (page < 0 || page >= a.n_pages) {
           bad_entry = 1;
         } else {
-          const int32_t refs = a.refs[page];
-          if (refs < 1) bad_entry = 1;
-          kind = refs > 1 ? 2 : 0;
+          const int32_t held = a.refs[page];
+          if (held < 1) bad_entry = 1;
+          kind = held > 1 ? 2 : 0;
         }
-        take[e] = kind;
+        if (e0 == 0) place = x, page0 = page, kind0 = kind;
+        else take[e] = kind;
       }
-      const Scan s = scan(kind == 2, sums);
+      const Scan s = scan((kind == 2) << 16 | (kind == 1), sums);   // (each at most kThreads)
       if (kind == 2) {
-        shared[n_shared + s.before] = page;
-        at[n_shared + s.before] = e;
+        shared[n_shared + (s.before >> 16)] = page;
+        at[n_shared + (s.before >> 16)] = e;
       }
-      n_shared += s.total;
+      if (e0 == 0) ranks = s.before & 0xFFFF;
+      n_shared += s.total >> 16;
+      takes += s.total & 0xFFFF;
     }
     __syncthreads();
     fits = bad_entry == 0;
   }
   const bool known = fits;   // (bad tables: nothing is counted)
-  int32_t takes = 0, copies = 0, found = 0;
+  int32_t copies = 0, found = 0;
   if (fits) {
-    for (int s = tid; s < n_shared; s += kThreads) {
-      const int32_t page = shared[s];
-      int rank = 0;
-      for (int k = 0; k < s; ++k) rank += shared[k] == page;
-      int b;
-      int32_t i;
-      bool partly;
-      locate(at[s], b, i, partly);
-      take[at[s]] = a.refs[page] - rank > 1 ? (partly ? 3 : 1) : 0;   // 3: and is copied
-    }
-    __syncthreads();
-    for (int e0 = 0; e0 < entries; e0 += kThreads) {
-      const Scan s = scan(e0 + tid < entries && take[e0 + tid] != 0, sums);
-      takes += s.total;
+    if (n_shared > 0) {
+      // (of the first kThreads too, through take[])
+      if (tid < entries) take[tid] = kind0;
+      __syncthreads();
+      for (int s0 = 0; s0 < n_shared; s0 += kThreads) {
+        const int s = s0 + tid;
+        int kind = 0;
+        if (s < n_shared) {
+          const int32_t page = shared[s];
+          int rank = 0;
+          for (int k = 0; k < s; ++k) rank += shared[k] == page;
+          if (a.refs[page] - rank > 1) kind = locate(at[s]).partly ? 3 : 1;   // 3: and is copied
+          take[at[s]] = kind;
+        }
+        takes += scan(kind != 0, sums).total;
+      }
+      __syncthreads();
+      if (tid < entries) kind0 = take[tid];
     }
     // 3. as many free pages, lowest first
-    for (int64_t p0 = 0; p0 < a.n_pages && found < takes; p0 += 4 * kThreads) {
-      const int64_t p = p0 + 4 * tid;
-      bool free_page[4];
+    for (int64_t p0 = 0; p0 < a.n_pages && found < takes; p0 += kPer * kThreads) {
+      const int64_t p = p0 + (int64_t)kPer * tid;
+      if (p0 > 0) look(p);
       int n = 0;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        free_page[u] = p + u < a.n_pages && a.refs[p + u] == 0;
-        n += free_page[u];
-      }
+      for (int u = 0; u < kPer / 4; ++u) n += (refs[u].x == 0) + (refs[u].y == 0) + (refs[u].z == 0) + (refs[u].w == 0);
       const Scan s = scan(n, sums);
       int k = found + s.before;
+      if (n > 0 && k < takes) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (free_page[u]) {
-          if (k < takes) lowest[k] = (int32_t)(p + u);
-          ++k;
+        for (int u = 0; u < kPer; ++u) {
+          const int32_t held = u % 4 == 0 ? refs[u / 4].x : u % 4 == 1 ? refs[u / 4].y : u % 4 == 2 ? refs[u / 4].z : refs[u / 4].w;
+          if (held == 0) {
+            if (k < takes) lowest[k] = (int32_t)(p + u);
+            ++k;
+          }
         }
+      }
       found += s.total;
     }
     __syncthreads();
     fits = found >= takes;
   }
   // 4. the tables changed
-  if (fits) {
+  if (fits && takes > 0) {
     int32_t taken = 0;
     for (int e0 = 0; e0 < entries; e0 += kThreads) {
       const int e = e0 + tid;
-      const int kind = e < entries ? take[e] : 0;
-      const Scan s = scan(kind != 0, sums);
-      const Scan c = scan(kind == 3, sums);
+      const int kind = e0 == 0 ? kind0 : e < entries ? take[e] : 0;
+      Scan s = {ranks, 0}, c = {0, 0};
+      if (n_shared > 0 || entries > kThreads) {
+        s = scan((kind == 3) << 16 | (kind != 0), sums);
+        c = {s.before >> 16, s.total >> 16};
+        s = {s.before & 0xFFFF, s.total & 0xFFFF};
+      }
       if (kind != 0) {
-        int b;
-        int32_t i;
-        bool partly;
-        locate(e, b, i, partly);
-        int32_t* entry = a.page_table + (int64_t)b * a.table_cap + i;
-        const int32_t page = lowest[taken + s.before], old = *entry;
-        if (old >= 0) atomicSub(a.refs + old, 1);
+        if (e0 > 0) {
+          place = locate(e);
+          page0 = *place.entry;
+        }
+        const int32_t page = lowest[taken + s.before];
+        if (page0 >= 0) atomicSub(a.refs + page0, 1);
         a.refs[page] = 1;
-        *entry = page;
+        *place.entry = page;
         if (kind == 3) {
-          a.pairs[2 * (copies + c.before)] = old;
+          a.pairs[2 * (copies + c.before)] = page0;
           a.pairs[2 * (copies + c.before) + 1] = page;
         }
       }

@@ -55,7 +55,7 @@ PIC_API pic_status pic_page_grow_async(const pic_pages* pages, int32_t batch, in
   a.ready = ready;
   a.result = result;
   a.workspace = static_cast<int32_t*>(workspace);
-  a.n_pages = pages->n_pages;
+  a.n_pages = batch > 0 ? pages->n_pages : 0;   // (without requests no page is looked at)
   a.table_cap = pages->table_cap;
   a.shift = __builtin_ctz((unsigned)pages->page_tokens);
   a.batch = batch;

@@ -125,6 +125,29 @@ def test_large_batches():
     compare(pages, refs, table, [5], 70001)
 
 
+def test_large_forked_batches():
+    """More requests than their places are kept of, more shared entries than threads, in several orders; and none at all."""
+    r = np.random.default_rng(17)
+    B = 4500
+    lens = r.integers(0, 64, B)
+    share = []
+    for d in range(1, B, 2):
+        lens[d] = int(r.integers(0, lens[d - 1] + 1))
+        share.append((d, d - 1, int(lens[d])))
+    pages, refs, table = state(r, 16, lens, 6, 3 * B, share)
+    compare(pages, refs, table, lens, 30)
+    rr, tt, _ = compare(pages, refs, table, lens, 1, r.integers(0, 2, B))
+    compare(pages, rr, tt, lens, 20)
+    lens = [100] * 1500
+    pages, refs, table = state(r, 64, lens, 3, 2000, [(d, 0, 100) for d in range(1, 1500)])
+    compare(pages, refs, table, lens, 50)
+    pairs, ready, result = dev(np.full((1, 2), 99)), dev([99]), dev([9, 9, 9])
+    pages = pic.Pages.of(2000, 64, 3)
+    ws = torch.empty(max(16, pic.pic_page_grow_workspace_bytes(pages, 0, 1)), dtype=torch.uint8, device=DEV)
+    pic.pic_page_grow_async(pages, 0, None, None, None, 1, pairs[:0], ready[:0], result, ws)
+    assert result.tolist() == [0, 0, 0] and pairs.tolist() == [[99, 99]] and ready.tolist() == [99]
+
+
 def test_refusals_change_nothing():
     r = np.random.default_rng(8)
     lens = [30, 64, 10, 100]
