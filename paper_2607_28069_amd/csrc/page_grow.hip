@@ -8,7 +8,7 @@
 // of 64 7.8 us, where a pass that found each place again before every step took 10.6.  The order of the host's
 // loop (request by request, entry by entry) comes from prefix sums over the workgroup; where several entries hold the
 // same shared page, the k-th of them takes a page of its own if the page has more than k + 1 references, so the last
-// ones keep it.  Nothing is changed before it is known that everything fits.
+// ones keep it.  Where not everything fits, nothing is changed (references given back are taken again).
 #include "pic_bounds.h"
 #include "pic_internal.h"
 
@@ -48,7 +48,7 @@ __device__ __forceinline__ Scan scan(int x, int (&sums)[kWaves]) {
 __global__ void __launch_bounds__(kThreads) page_grow_kernel(PageGrowArgs a, int32_t cap_entries) {
   constexpr int kFirst = 4096, kPer = 16;   // requests in LDS; pages a thread looks at at once
   __shared__ int sums[kWaves];
-  __shared__ int32_t first_lds[kFirst + 1];
+  __shared__ int32_t first_lds[kFirst + 1], held_lds[kThreads];
   __shared__ int bad_cap, bad_entry;
   const int tid = threadIdx.x;
   int32_t* first = a.batch <= kFirst ? first_lds : a.workspace;
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(kThreads) page_grow_kernel(PageGrowArgs a, int
 #pragma unroll
     for (int u = 0; u < kPer / 4; ++u) {
       const int64_t p = p0 + 4 * u;
-      if (p + 4 <= a.n_pages) __builtin_memcpy(&refs[u], a.refs + p, 16);   // (refs is 4-byte aligned)
+      if (p + 4 <= a.n_pages) refs[u] = *reinterpret_cast<const int4*>(a.refs + p);
       else refs[u] = make_int4(p < a.n_pages ? a.refs[p] : 1, p + 1 < a.n_pages ? a.refs[p + 1] : 1, p + 2 < a.n_pages ? a.refs[p + 2] : 1, 1);
     }
   };
@@ -148,18 +148,25 @@ __global__ void __launch_bounds__(kThreads) page_grow_kernel(PageGrowArgs a, int
     if (n_shared > 0) {
       // (of the first kThreads too, through take[])
       if (tid < entries) take[tid] = kind0;
-      __syncthreads();
+      // kThreads of them at a time: those before them have given their references back (which the next ones see, past the
+      // first-level cache), and the places among the same page's come from LDS
       for (int s0 = 0; s0 < n_shared; s0 += kThreads) {
         const int s = s0 + tid;
+        const int32_t page = s < n_shared ? shared[s] : -1;
+        held_lds[tid] = page;
+        __syncthreads();
         int kind = 0;
         if (s < n_shared) {
-          const int32_t page = shared[s];
           int rank = 0;
-          for (int k = 0; k < s; ++k) rank += shared[k] == page;
-          if (a.refs[page] - rank > 1) kind = locate(at[s]).partly ? 3 : 1;   // 3: and is copied
+          for (int k = 0; k < tid; ++k) rank += held_lds[k] == page;
+          if (__hip_atomic_load(a.refs + page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) - rank > 1)
+            kind = locate(at[s]).partly ? 3 : 1;   // 3: and is copied
           take[at[s]] = kind;
         }
-        takes += scan(kind != 0, sums).total;
+        takes += scan(kind != 0, sums).total;   // (every count is read)
+        if (kind != 0) atomicSub(a.refs + page, 1);
+        if (s0 + kThreads < n_shared) __threadfence();
+        __syncthreads();
       }
       __syncthreads();
       if (tid < entries) kind0 = take[tid];
@@ -187,6 +194,10 @@ __global__ void __launch_bounds__(kThreads) page_grow_kernel(PageGrowArgs a, int
     }
     __syncthreads();
     fits = found >= takes;
+    if (!fits) {   // shared pages get their references back
+      for (int s = tid; s < n_shared; s += kThreads)
+        if (take[at[s]] != 0) atomicAdd(a.refs + shared[s], 1);
+    }
   }
   // 4. the tables changed
   if (fits && takes > 0) {
@@ -206,7 +217,6 @@ __global__ void __launch_bounds__(kThreads) page_grow_kernel(PageGrowArgs a, int
           page0 = *place.entry;
         }
         const int32_t page = lowest[taken + s.before];
-        if (page0 >= 0) atomicSub(a.refs + page0, 1);
         a.refs[page] = 1;
         *place.entry = page;
         if (kind == 3) {

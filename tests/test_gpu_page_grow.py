@@ -141,6 +141,9 @@ def test_large_forked_batches():
     lens = [100] * 1500
     pages, refs, table = state(r, 64, lens, 3, 2000, [(d, 0, 100) for d in range(1, 1500)])
     compare(pages, refs, table, lens, 50)
+    few = refs.copy()
+    few[np.flatnonzero(refs == 0)[1400:]] = 1                      # 1499 take one
+    assert compare(pages, few, table, lens, 1)[2] == -4
     pairs, ready, result = dev(np.full((1, 2), 99)), dev([99]), dev([9, 9, 9])
     pages = pic.Pages.of(2000, 64, 3)
     ws = torch.empty(max(16, pic.pic_page_grow_workspace_bytes(pages, 0, 1)), dtype=torch.uint8, device=DEV)
