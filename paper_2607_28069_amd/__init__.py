@@ -648,6 +648,8 @@ def pic_page_grow_async(pages: Pages, batch, refs, page_table, base_len, n_new, 
 
 def pic_page_copy_async(model: Model, pages: Pages, pages_k, pages_v, pairs, pair_cap, stream=None):
     """pairs: device int32 [pair_cap][2] (source, destination) pages; entries that are no pages are skipped."""
+    if str(pairs.dtype) != "torch.int32" or pairs.numel() < 2 * pair_cap:
+        raise ValueError(f"pairs: {2 * pair_cap} int32 entries expected, got {pairs.numel()} of {pairs.dtype}")
     (k, v, pr), st = _on_device((pages_k, pages_v, pairs), stream)
     _check(load().pic_page_copy_async(ctypes.byref(model), ctypes.byref(pages), k, v, pr, int(pair_cap), st))
 

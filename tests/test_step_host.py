@@ -92,6 +92,23 @@ def test_shared_workspace_query():
     assert q(m=pic.Model.of(1, 4, 2, 80, "bf16", 1e4)) == 0
 
 
+@pytest.mark.parametrize("model", [(1, 32, 8, 128), (2, 28, 4, 128), (1, 4, 2, 64), (32, 32, 8, 128)])
+def test_one_workspace_serves_a_decode_loop(model):
+    """What is asked for at the end of a loop is enough at every step before it."""
+    m = pic.Model.of(*model, "bf16", 1e4)
+    for groups, batch, n in ((pic.Shared.of(1, 2, 2048), 2, 1), (pic.Shared.of(4, 12, 8192), 37, 1), (pic.Shared.of(70, 3, 640), 140, 1),
+                             (pic.Shared.of(1, 64, 16384), 64, 1), (pic.Shared.of(2, 8, 0), 16, 3), (pic.Shared.of(1, 16, 1000), 16, 131)):
+        sizes = [pic.pic_page_shared_workspace_bytes(m, groups, batch, n, c) for c in [*range(0, 700), *range(701, 20000, 61)]]
+        assert sizes == sorted(sizes) and sizes[0] > 0
+
+
+def test_copy_listed_binding_refusals():
+    model, pages = pic.Model.of(1, 2, 2, 64, "f32", 1e4), pic.Pages.of(4, 16, 0)
+    for pairs in (torch.zeros((2, 2), dtype=torch.int32), torch.zeros((3, 2), dtype=torch.int64)):
+        with pytest.raises(ValueError, match="pairs"):
+            pic.pic_page_copy_async(model, pages, None, None, pairs, 3)
+
+
 def test_grow_refusals(p):
     def call(pages=pic.Pages.of(8, 16, 4), batch=2, refs=p, table=p, lens=p, offset=0, nv=None, n=3, pairs=p, ready=p, result=p, ws=p,
              ws_bytes=1 << 12):
