@@ -295,3 +295,24 @@ def test_bad_tables_stay_in_bounds():
         suffix(x)
         torch.cuda.synchronize()
         assert (x.pk.view(torch.int16) == before.view(torch.int16)).all()
+
+
+@pytest.mark.parametrize("sizes", [[1, 2, 1] * 24, [1] * 63 + [3], [2] * 62])
+def test_many_groups(sizes):
+    """Starts that one wave holds, and more of them."""
+    B = sum(sizes)
+    shared = [64 + 64 * (i % 3) + (i % 5) for i in range(len(sizes))]
+    ctx = np.concatenate([[s + i + (7 * i) % 90 for i in range(n)] for n, s in zip(sizes, shared)]).tolist()
+    x = batch(4, 2, 64, 16, ctx, [1] * B, starts(sizes), shared)
+    decode(x)
+    right(x)
+
+
+@pytest.mark.parametrize("hq,hkv,d,L", [(16, 16, 128, 2), (64, 8, 128, 3)])
+def test_a_batch_past_the_last_level_cache(hq, hkv, d, L):
+    """Rows of more than 256 MB pass the caches by: the same outputs, from a plan of its own."""
+    ctx, n_groups = [8200, 8300, 8400, 8500, 8600, 8700, 8800, 8900], 4
+    x = batch(hq, hkv, d, 64, ctx, [1] * 8, [0, 2, 4, 6, 8], [8200, 8300, 8500, 8700], L=L)
+    assert x.pk.numel() * 4 > 300e6
+    decode(x)
+    right(x)
