@@ -479,10 +479,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
     part_of<HD, 1, 2, false, kStream>(a, blockIdx.x - a.prefix_blocks, lds);
 }
 
-// The parts of a query row joined, where they are few: HD / 4 lanes a row, all parts' loads on their way at once.  (With
-// more parts than that, the combine of page_decode.hip: a workgroup a row.)
-constexpr int kFewParts = 8;
-template <int HD>
+// The parts of a query row joined, where they are few: HD / 4 lanes a row, all parts' loads on their way at once.
+template <int HD, int kFewParts>
 __global__ void __launch_bounds__(256) shared_combine_kernel(PageSharedArgs a, bf16_t* __restrict__ out, int64_t n_rows) {
   constexpr int kLanes = HD / 4;
   const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
@@ -494,10 +492,12 @@ __global__ void __launch_bounds__(256) shared_combine_kernel(PageSharedArgs a, b
   float2 ml[kFewParts];
   f32x4_t x[kFewParts];
 #pragma unroll
-  for (int u = 0; u < kFewParts; ++u) {   // (past the last one: that one again, with a weight of 0)
-    const int s = min(u, parts - 1);
-    ml[u] = pml[s];
-    x[u] = *reinterpret_cast<const f32x4_t*>(po + (int64_t)s * HD);
+  for (int u = 0; u < kFewParts; ++u) {   // (past the last one of up to 8: that one again, with a weight of 0)
+    const int s = kFewParts > 8 ? u : min(u, parts - 1);
+    if (kFewParts == 8 || s < parts) {
+      ml[u] = pml[s];
+      x[u] = *reinterpret_cast<const f32x4_t*>(po + (int64_t)s * HD);
+    }
   }
   if (tok - lb * a.n_new >= page_new_tokens(a.base_len, a.n_valid, (int)(lb % a.batch), a.n_new)) return;   // padding
   float M = kNoMax, den = 0.f;
@@ -526,10 +526,14 @@ hipError_t launch_hd(const PageSharedArgs& a, const SharedPlan& plan, dim3 grid,
   hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  // Few parts, or more rows than workgroups fit the GPU at once (2 layers of 12 x 5 tokens, 32 heads of 64, 9 parts: 27.2 -> 25
+  // us for the call; 224 rows of 16 parts 8.9 -> 9.3): lanes a row.  Else the combine of page_decode.hip, a workgroup a row
+  // (512 rows of 28 parts 19.8 us, 21.0 the other way).
   const int parts = a.prefix_splits + a.own_splits;
-  if (parts <= kFewParts) {
-    const int64_t rows = (int64_t)s.n_layers * s.batch * a.n_new * s.n_q_heads;
-    hipLaunchKernelGGL((shared_combine_kernel<HD>), dim3((unsigned)((rows * (HD / 4) + 255) / 256)), dim3(256), 0, stream, a, out, rows);
+  const int64_t row_count = (int64_t)s.n_layers * s.batch * a.n_new * s.n_q_heads;
+  if (parts <= 8 || (parts <= 16 && row_count >= 2048)) {
+    const auto join = parts <= 8 ? shared_combine_kernel<HD, 8> : shared_combine_kernel<HD, 16>;
+    hipLaunchKernelGGL(join, dim3((unsigned)((row_count * (HD / 4) + 255) / 256)), dim3(256), 0, stream, a, out, row_count);
     return hipGetLastError();
   }
   AttnShape rows = s;   // (the combine's rows of a request: every head of every token)

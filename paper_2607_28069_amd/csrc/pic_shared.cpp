@@ -36,10 +36,13 @@ int64_t ceil_of(int64_t n, int64_t d) { return (n + d - 1) / d; }
 
 }  // namespace
 
-// Key ranges of a launch: as many as cover the compute units once, one and a half times, or twice, whichever the estimate
-// above puts first, requests' own ranges filling what is left.  Measured, us by ranges of the prefix (head_dim 128, 8 kv heads):
+// Key ranges of a launch: as many as cover some or all compute units, or up to twice, whichever the estimate above puts first
+// (few where a prefix is short and its rows many, as each range writes a part of every row, which the combine reads), requests'
+// own ranges filling what is left.  Measured, us by ranges of the prefix (head_dim 128, 8 kv heads):
 // 64 requests over 16K + 300 own (16 workgroups a range) 16: 41.5, 24: 47, 32: 49; 16 over 10K (8) 20: 21.3, 28: 19.0, 40:
-// 22.1; 16 x 24 tokens over 10K (96) 2: 143, 4: 92, 5: 86, 8: 107; 4 groups of up to 32K (16) 16: 63, 24: 60, 28: 57.
+// 22.1; 16 x 24 tokens over 10K (96) 2: 143, 4: 92, 5: 86, 8: 107; 4 groups of up to 32K (16) 16: 63, 24: 60, 28: 55 (at
+// head_dim 64, or with 64 rows at most, such a share of the second place on every compute unit loses 1 to 2 us); 32 over 2K
+// (8) 31: 20.2, 16: 17.8; 4 x 4 tokens over 2K (8) 31: 15.3, 16: 12.8; 16 over 2K (8) 31: 14.5, 16: 12.7.
 SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, int32_t max_ctx) {
   SharedPlan p;
   const int64_t n_rep = s.n_q_heads / s.n_kv_heads;
@@ -60,10 +63,11 @@ SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, in
   cost.own_units = own_units;
   // (bound by the loads, which one workgroup with tiles of half the size does not keep busy, or by products)
   cost.both = p.row_blocks == 2 ? 1.7 : s.head_dim == 64 ? 1.3 : 2.0;
-  cost.join = (double)part_bytes * 2.0 / 4.8e6;
+  cost.join = (double)part_bytes * 2.0 / 5.8e6;   // (written and read, 4.8 TB/s)
   double best = 1e30;
-  for (const int64_t fill : {256, 384, 512}) {
-    if (fill == 256 && m.n_groups > 1) continue;   // (nor of one length: longer ones need company)
+  for (const int64_t fill : {32, 64, 96, 128, 192, 256, 384, 448, 512}) {
+    if (fill < 384 && m.n_groups > 1) continue;   // (nor of one length: longer ones need company)
+    if (fill == 448 && (p.row_blocks == 1 || s.head_dim == 64)) continue;
     int64_t n = 0, tiles = 0;
     if (prefix_tiles > 0 && prefix_units > 0) {
       n = std::min({std::max<int64_t>(1, fill / cost.prefix_units), prefix_tiles, (int64_t)kSharedMaxSplits});
