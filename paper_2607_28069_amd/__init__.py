@@ -626,9 +626,13 @@ def pic_page_grow_workspace_bytes(pages: Pages, batch, n_new) -> int:
     return load().pic_page_grow_workspace_bytes(ctypes.byref(pages), int(batch), int(n_new))
 
 
-def _device_i32(t, n, name):
-    if t is not None and (str(t.dtype) != "torch.int32" or t.numel() != n):
-        raise ValueError(f"{name}: {n} int32 entries expected, got {t.numel()} of {t.dtype}")
+def _device_i32(*sizes):
+    """Tensors (or None) hold the int32 entries that they must: (tensor, entries, name) each."""
+    import torch
+    i32 = torch.int32
+    for t, n, name in sizes:
+        if t is not None and (t.dtype is not i32 or t.numel() != n):
+            raise ValueError(f"{name}: {n} int32 entries expected, got {t.numel()} of {t.dtype}")
 
 
 def pic_page_grow_async(pages: Pages, batch, refs, page_table, base_len, n_new, pairs, ready, result, workspace, n_valid=None,
@@ -636,10 +640,8 @@ def pic_page_grow_async(pages: Pages, batch, refs, page_table, base_len, n_new, 
     """pic_page_grow on the device, for the tokens that an attention call with these base_len, offset, n_valid and n_new
     stores: refs [n_pages] and page_table [batch][table_cap] are updated, pairs [batch][2], ready [batch] (base_len for that
     call, -1 where this one fails) and result [3] (status, pairs, pages taken) written; device int32 tensors."""
-    for t, n, name in ((refs, pages.n_pages, "refs"), (page_table, batch * pages.table_cap, "page_table"),
-                       (base_len, batch, "base_len"), (n_valid, batch, "n_valid"), (pairs, 2 * batch, "pairs"),
-                       (ready, batch, "ready"), (result, 3, "result")):
-        _device_i32(t, n, name)
+    _device_i32((refs, pages.n_pages, "refs"), (page_table, batch * pages.table_cap, "page_table"), (base_len, batch, "base_len"),
+                (n_valid, batch, "n_valid"), (pairs, 2 * batch, "pairs"), (ready, batch, "ready"), (result, 3, "result"))
     (rf, tab, lens, nv, pr, rd, rs, ws), st = _on_device((refs, page_table, base_len, n_valid, pairs, ready, result, workspace),
                                                          stream)
     _check(load().pic_page_grow_async(ctypes.byref(pages), int(batch), rf, tab, lens, int(offset), nv, int(n_new), pr, rd, rs, ws,
