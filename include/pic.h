@@ -563,8 +563,8 @@ pic_status pic_page_decode_attn_rope(const pic_model* model, const pic_pages* pa
      max_len                     bound on shared_len (clamped to it); <= table_cap * page_tokens
      group_start [device, n_groups + 1]  increasing; NULL: one group, the whole batch (n_groups 1)
      shared_len  [device, n_groups]
-     workspace                   pic_page_shared_workspace_bytes(...) bytes for the same model, groups, batch and n_new
-                                 (decode: 1) and this max_ctx (decode: max_base_len + step) or a larger one
+     workspace                   pic_page_shared_workspace_bytes(...) bytes for the same model, n_groups and max_group, and
+                                 these or larger max_len, batch, n_new (decode: 1) and max_ctx (decode: max_base_len + step)
    (the other arguments, padding, what is stored and what is not finite as for pic_page_suffix_attn and
    pic_page_decode_attn; queries and keys rotated; n_suffix * Hkv below 2^24.)  Probabilities over a request's own slots
    keep 16 bits, those over shared ones too where max_group * n_suffix * Hq / Hkv is 64 or less, and 8 otherwise.  Last

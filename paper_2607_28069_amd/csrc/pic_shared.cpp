@@ -89,12 +89,17 @@ SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, in
   // Rows that the last-level cache (256 MB) will not hold until the next call leave it to others (8 requests x 33K in 4
   // groups 60 -> 55 us, 64 requests of up to 2K of their own 72 -> 63; below, 16 over 10K 19.5 -> 21.2).
   p.stream = p.prefix_row_tiles <= 1 && heads * s.head_dim * 4.0 * ((double)m.n_groups * prefix_tiles + (double)s.batch * own_tiles) * kSharedKeys > 256e6;
-  // room for the parts of any plan for up to max_ctx slots, so that one workspace serves a decode loop
-  const int64_t most_prefix = prefix_tiles > 0 && prefix_units > 0
-                                  ? std::min({std::max<int64_t>(1, 512 / cost.prefix_units), prefix_tiles, (int64_t)kSharedMaxSplits}) : 0;
-  const int64_t most_tiles = std::max(own_tiles, ceil_of((int64_t)kSharedKeys - 1 + n_new, kSharedKeys));   // (all slots but a tile's shared)
-  const int64_t most_own = std::max<int64_t>(1, std::min({512 / own_units, (most_tiles + 1) / 2, (int64_t)kSharedMaxSplits}));
-  p.ws_bytes = (size_t)(part_bytes * (most_prefix + most_own));
+  // Room for every call of these groups with no more requests, tokens and slots, so that a buffer for the largest serves all.
+  // Parts of prefixes: max(1, 512 / prefix_units) ranges of R = heads * batch * own_rows rows, where prefix_units / heads is at
+  // least 1, batch * own_rows / 128, or n_groups * max_group * own_rows / 128.  Of requests: max(1, 512 / own_units), where
+  // own_units / heads is at least batch, or batch * own_rows / 64.
+  const int64_t grouped = (int64_t)m.n_groups * m.max_group;
+  int64_t most = 0;
+  if (prefix_tiles > 0 && grouped > 0)
+    most = std::max(rows, std::min({65536 * ceil_of(s.batch, grouped), 512 * s.batch * own_rows, rows * std::min<int64_t>(prefix_tiles, kSharedMaxSplits)}));
+  const int64_t all_tiles = ceil_of((int64_t)max_ctx + n_new, kSharedKeys);
+  most += std::max(rows, std::min(512 * std::min<int64_t>(64, own_rows), rows * std::min<int64_t>((all_tiles + 1) / 2, kSharedMaxSplits)));
+  p.ws_bytes = (size_t)most * (s.head_dim + 2) * sizeof(float);
   return p;
 }
 

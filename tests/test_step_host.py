@@ -92,14 +92,18 @@ def test_shared_workspace_query():
     assert q(m=pic.Model.of(1, 4, 2, 80, "bf16", 1e4)) == 0
 
 
-@pytest.mark.parametrize("model", [(1, 32, 8, 128), (2, 28, 4, 128), (1, 4, 2, 64), (32, 32, 8, 128)])
-def test_one_workspace_serves_a_decode_loop(model):
-    """What is asked for at the end of a loop is enough at every step before it."""
+@pytest.mark.parametrize("model", [(1, 32, 8, 128), (2, 28, 4, 128), (1, 4, 2, 64), (32, 32, 8, 128), (1, 1, 1, 64)])
+def test_one_workspace_serves_smaller_calls(model):
+    """What is asked for at the largest sizes is enough at every size before them: each step of a decode loop, fewer requests,
+    fewer tokens, shorter prefixes."""
     m = pic.Model.of(*model, "bf16", 1e4)
-    for groups, batch, n in ((pic.Shared.of(1, 2, 2048), 2, 1), (pic.Shared.of(4, 12, 8192), 37, 1), (pic.Shared.of(70, 3, 640), 140, 1),
-                             (pic.Shared.of(1, 64, 16384), 64, 1), (pic.Shared.of(2, 8, 0), 16, 3), (pic.Shared.of(1, 16, 1000), 16, 131)):
-        sizes = [pic.pic_page_shared_workspace_bytes(m, groups, batch, n, c) for c in [*range(0, 700), *range(701, 20000, 61)]]
-        assert sizes == sorted(sizes) and sizes[0] > 0
+    for groups, batch, n in (((1, 2, 2048), 2, 1), ((4, 12, 8192), 37, 1), ((70, 3, 640), 140, 1), ((1, 64, 16384), 64, 1), ((2, 8, 0), 16, 3),
+                             ((1, 16, 1000), 16, 131), ((2, 0, 500), 4, 1), ((1, 3, 4000), 200, 2)):
+        need = lambda b=batch, t=n, s=groups[2], c=20000: pic.pic_page_shared_workspace_bytes(  # noqa: E731
+            m, pic.Shared.of(*groups[:2], s), b, t, c)
+        for sizes in ([need(c=c) for c in [*range(0, 700), *range(701, 20000, 61)]], [need(b=b) for b in range(1, batch + 1)],
+                      [need(t=t) for t in range(1, n + 1)], [need(s=s) for s in range(0, groups[2] + 1, 16)]):
+            assert sizes == sorted(sizes) and sizes[0] > 0
 
 
 def test_copy_listed_binding_refusals():
