@@ -554,11 +554,12 @@ pic_status pic_page_decode_attn_rope(const pic_model* model, const pic_pages* pa
    requests together, instead of once per request.
    The requests of a group are neighbours in the batch: group i holds requests [group_start[i], group_start[i + 1])
    and shares slots [0, shared_len[i]), read through the page table row of its first request.  That request may be padding of
-   the batch (one that holds the prefix): nothing else of it is read then.  The other requests' tables must name pages
+   the batch (one that holds the prefix): nothing else of it is read then.  Its new tokens come after the shared slots, and no
+   request's into a page that others hold (pic_page_grow sees to that).  The other requests' tables must name pages
    that hold the same there (pic_page_fork's do).  A request whose new tokens come before the end of the shared slots sees its own
    slots only, [0, p], as always; the last shared_len[i] % 64 shared slots are read by each request.  Requests in no group
    share nothing.
-     n_groups                    >= 1
+     n_groups                    >= 1, below 2^24
      max_group                   bound on the requests of a group: those past it in their group share nothing
      max_len                     bound on shared_len (clamped to it); <= table_cap * page_tokens
      group_start [device, n_groups + 1]  increasing; NULL: one group, the whole batch (n_groups 1)

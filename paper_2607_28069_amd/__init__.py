@@ -604,6 +604,7 @@ def pic_page_shared_suffix_attn(model: Model, pages: Pages, shared: Shared, q, k
                                 batch, group_start, shared_len, ctx_len, max_ctx, n_suffix, out, workspace=None, n_valid=None,
                                 scale=0.0, stream=None):
     """group_start: device int32 [n_groups + 1], or None (one group); shared_len: device int32 [n_groups]."""
+    _device_i32((group_start, shared.n_groups + 1, "group_start"), (shared_len, shared.n_groups, "shared_len"))
     (*a, tab, gs, sl, lens, nv, o, ws), st = _on_device((q, k_suf, v_suf, pages_k, pages_v, page_table, group_start, shared_len,
                                                          ctx_len, n_valid, out, workspace), stream)
     _check(load().pic_page_shared_suffix_attn(ctypes.byref(model), ctypes.byref(pages), ctypes.byref(shared), *a, tab, int(batch),
@@ -615,6 +616,7 @@ def pic_page_shared_decode_attn(model: Model, pages: Pages, shared: Shared, q, k
                                 batch, group_start, shared_len, base_len, step, max_base_len, out, workspace=None, scale=0.0,
                                 stream=None):
     """group_start: device int32 [n_groups + 1], or None (one group); shared_len: device int32 [n_groups]."""
+    _device_i32((group_start, shared.n_groups + 1, "group_start"), (shared_len, shared.n_groups, "shared_len"))
     (*a, tab, gs, sl, lens, o, ws), st = _on_device((q, k_new, v_new, pages_k, pages_v, page_table, group_start, shared_len,
                                                      base_len, out, workspace), stream)
     _check(load().pic_page_shared_decode_attn(ctypes.byref(model), ctypes.byref(pages), ctypes.byref(shared), *a, tab, int(batch),

@@ -289,7 +289,7 @@ hipError_t launch_page_grow(const PageGrowArgs& a, hipStream_t stream) {
 hipError_t launch_page_copy_listed(void* pages_k, void* pages_v, int64_t n_streams, int64_t n_pages, int64_t page_bytes,
                                    const int32_t* pairs, int32_t cap, hipStream_t stream) {
   const int64_t page16 = page_bytes / 16;
-  const unsigned grid = (unsigned)std::min<int64_t>((int64_t)cap * 2 * n_streams, 2048);
+  const unsigned grid = (unsigned)std::min<int64_t>((int64_t)cap * 2 * std::min<int64_t>(n_streams, 2048), 2048);
   hipLaunchKernelGGL(page_copy_listed_kernel, dim3(grid), dim3(256), 0, stream, static_cast<u32x4*>(pages_k),
                      static_cast<u32x4*>(pages_v), n_streams, n_pages * page16, (int32_t)page16,
                      reinterpret_cast<const int2*>(pairs), cap, (int32_t)n_pages);

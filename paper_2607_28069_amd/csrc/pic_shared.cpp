@@ -124,7 +124,8 @@ pic_status check_sizes(const pic_model* m, const pic_shared* sh, int32_t batch, 
                        SharedPlan* plan) {
   if (batch < 0 || n_new < 0 || max_ctx < 0) return fail(PIC_ERR_INVALID_ARG, "negative size");
   if (max_ctx + n_new > kMaxSlots) return fail(PIC_ERR_CAPACITY, "%lld slots per request (at most 2^30)", (long long)max_ctx + n_new);
-  if ((int64_t)batch * m->n_q_heads * n_new * std::max(m->n_layers, 1) >= (int64_t(1) << 27)) return fail(PIC_ERR_UNSUPPORTED, "too many query rows");
+  if (sh->n_groups >= 1 << 24) return fail(PIC_ERR_UNSUPPORTED, "too many groups");
+  if ((double)batch * m->n_q_heads * n_new * std::max(m->n_layers, 1) >= (double)(1 << 27)) return fail(PIC_ERR_UNSUPPORTED, "too many query rows");
   if ((int64_t)n_new * m->n_kv_heads >= (int64_t(1) << 24)) return fail(PIC_ERR_UNSUPPORTED, "too many new tokens per request");
   if (m->n_layers > 65535) return fail(PIC_ERR_UNSUPPORTED, "more than 65535 layers");
   groups->n_groups = sh->n_groups;

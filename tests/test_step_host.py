@@ -73,6 +73,9 @@ def test_shared_refusals(p, decode):
     assert call(batch=0, q=None) == 0
     assert call(model=M.of(0, 4, 2, 64, "bf16", 1e4)) == 0
     assert call(batch=1 << 30) == UNSUPPORTED
+    assert call(groups=S.of(1 << 24, 2, 20)) == UNSUPPORTED
+    many = 2**31 - 1
+    assert call(batch=many, model=M.of(many, many, 1, 64, "bf16", 1e4)) == UNSUPPORTED
     if decode:
         assert call(step=-1) == INVALID
         assert call(step=60) == CAPACITY
@@ -104,6 +107,17 @@ def test_one_workspace_serves_smaller_calls(model):
         for sizes in ([need(c=c) for c in [*range(0, 700), *range(701, 20000, 61)]], [need(b=b) for b in range(1, batch + 1)],
                       [need(t=t) for t in range(1, n + 1)], [need(s=s) for s in range(0, groups[2] + 1, 16)]):
             assert sizes == sorted(sizes) and sizes[0] > 0
+
+
+def test_shared_binding_refusals():
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    pages, groups = pic.Pages.of(8, 16, 4), pic.Shared.of(2, 2, 20)
+    for start, length, name in ((i32(2), i32(2), "group_start"), (i32(3).long(), i32(2), "group_start"), (i32(3), i32(1), "shared_len"),
+                                (i32(3), i32(2).float(), "shared_len")):
+        with pytest.raises(ValueError, match=name):
+            pic.pic_page_shared_decode_attn(MODEL, pages, groups, None, None, None, None, None, None, 2, start, length, None, 0, 10, None)
+        with pytest.raises(ValueError, match=name):
+            pic.pic_page_shared_suffix_attn(MODEL, pages, groups, None, None, None, None, None, None, 2, start, length, None, 10, 1, None)
 
 
 def test_copy_listed_binding_refusals():
