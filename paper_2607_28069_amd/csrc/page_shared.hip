@@ -14,9 +14,9 @@
 //    to its limit; tiles that some row of the workgroup sees in part are masked, and values there that are not finite
 //    cleared in LDS, so that rows that do not see them stay as they are (the others get them back at the end).
 //
-// Measured (combine included, 32 + 2 x 8 heads of 128): 2 requests over 2K 10 us, 16 over 10K 20, 64 over 16K 43, each about 1.2
+// Measured (combine included, 32 + 2 x 8 heads of 128): 2 requests over 2K 10 us, 16 over 10K 19.6, 64 over 16K 42, each about 1.2
 // us a tile of 64 keys that a workgroup has to itself, the first one after 4 to 5 where all start at once; 37 requests in
-// 4 groups of up to 32K (28 + 2 x 4 heads) 52 us, 4.2 TB/s in all; 16 x 24 tokens over 10K 81 us, 815 TFLOP/s.
+// 4 groups of up to 32K (28 + 2 x 4 heads) 51 us, 4.3 TB/s in all; 16 x 24 tokens over 10K 79 us, 820 TFLOP/s.
 #include <type_traits>
 
 #include "decode_common.h"

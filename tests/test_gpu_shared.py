@@ -316,3 +316,15 @@ def test_a_batch_past_the_last_level_cache(hq, hkv, d, L):
     assert x.pk.numel() * 4 > 300e6
     decode(x)
     right(x)
+
+
+@pytest.mark.parametrize("hq,hkv,d,L,sizes,n,shared", [(32, 8, 64, 2, [6, 6], 5, 1200), (32, 8, 128, 2, [4, 4], 4, 3000), (32, 8, 128, 1, [16], 8, 2000),
+                                                       (8, 2, 128, 1, [8], 9, 2000), (32, 8, 128, 2, [8, 8], 9, 900)])
+def test_parts_joined_in_every_way(hq, hkv, d, L, sizes, n, shared):
+    """Few parts of many rows, some of many, many of few; requests of a group that others do not fill."""
+    B = sum(sizes)
+    ctx = [shared + (13 * b) % 50 for b in range(B)]
+    ctx[-1] = 70
+    x = batch(hq, hkv, d, 64, ctx, [1 + (b % n) for b in range(B)], starts(sizes), [shared] * len(sizes), n=n, L=L)
+    suffix(x)
+    right(x)
