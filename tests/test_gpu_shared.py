@@ -328,3 +328,25 @@ def test_parts_joined_in_every_way(hq, hkv, d, L, sizes, n, shared):
     x = batch(hq, hkv, d, 64, ctx, [1 + (b % n) for b in range(B)], starts(sizes), [shared] * len(sizes), n=n, L=L)
     suffix(x)
     right(x)
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, each with a workspace of its own, several times over."""
+    xs = [batch(32, 8, 128, 64, [1500, 1400, 1333, 1800], [1] * 4, [0, 4], [1333]),
+          batch(32, 8, 128, 32, [900, 910, 905, 950, 64, 77], [3] * 6, [0, 4, 6], [900, 64], n=3, seed=1)]
+    want = [decode(xs[0]).clone(), suffix(xs[1]).clone()]
+    ws = [workspace(x, x.n, x.max_ctx) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    for it in range(5):
+        for x in xs:
+            x.out.fill_(SENTINEL)
+        torch.cuda.synchronize()
+        for _ in range(4):
+            with torch.cuda.stream(streams[0]):
+                decode(xs[0], ws=ws[0])
+            with torch.cuda.stream(streams[1]):
+                suffix(xs[1], ws=ws[1])
+        torch.cuda.synchronize()
+        assert all((x.out == w).all() for x, w in zip(xs, want)), it
+    for x in xs:
+        right(x)
