@@ -567,9 +567,9 @@ pic_status pic_page_decode_attn_rope(const pic_model* model, const pic_pages* pa
      workspace                   pic_page_shared_workspace_bytes(...) bytes for the same model, n_groups and max_group, and
                                  these or larger max_len, batch, n_new (decode: 1) and max_ctx (decode: max_base_len + step)
    (the other arguments, padding, what is stored and what is not finite as for pic_page_suffix_attn and
-   pic_page_decode_attn; queries and keys rotated; n_suffix * Hkv below 2^24.)  Probabilities over a request's own slots
-   keep 16 bits, those over shared ones too where max_group * n_suffix * Hq / Hkv is 64 or less, and 8 otherwise.  Last
-   bits depend on the batch and on the bounds, which set the key ranges of the launch, never on the lengths of other
+   pic_page_decode_attn; queries and keys rotated; n_suffix * Hkv below 2^24.)  Probabilities keep
+   16 bits; but over shared slots 8 where a request has more than 32 query rows per kv head (n_suffix * Hq / Hkv) and a group,
+   of max_group requests, more than 64.  Last bits depend on the batch and on the bounds, which set the key ranges of the launch, never on the lengths of other
    requests.  On float32 pages the calls are those two, request by
    request, and need no workspace. */
 typedef struct {

@@ -480,8 +480,9 @@ __device__ __forceinline__ void part_of(const PageSharedArgs& a, int block, cons
   }
 }
 
-// grid (prefix_blocks + own blocks, L), 256 threads; NB blocks of 16 rows a wave over the prefixes
-template <int HD, int NB, bool kStream>
+// grid (prefix_blocks + own blocks, L), 256 threads; NB blocks of 16 rows a wave over the prefixes, kTerms terms of a
+// probability there
+template <int HD, int NB, int kTerms, bool kStream>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) page_shared_kernel(PageSharedArgs a) {
   constexpr int kTileBytes = kKeys * Dims<HD>::kRowBytes;
   // (arrays of their own, so that the compiler sees that moves into one do not alias reads of another)
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   __shared__ int odd;
   const Buffers lds = {k_lds0, k_lds1, v_lds0, v_lds1, &odd};
   if ((int)blockIdx.x < a.prefix_blocks)
-    part_of<HD, NB, NB == 1 ? 2 : 1, true, kStream>(a, blockIdx.x, lds);
+    part_of<HD, NB, kTerms, true, kStream>(a, blockIdx.x, lds);
   else
     part_of<HD, 1, 2, false, kStream>(a, blockIdx.x - a.prefix_blocks, lds);
 }
@@ -536,9 +537,9 @@ __global__ void __launch_bounds__(256) shared_combine_kernel(PageSharedArgs a, b
 
 template <int HD>
 hipError_t launch_hd(const PageSharedArgs& a, const SharedPlan& plan, dim3 grid, const AttnShape& s, bf16_t* out, hipStream_t stream) {
-  const bool two = plan.row_blocks == 2;
-  const auto kernel = two ? (plan.stream ? page_shared_kernel<HD, 2, true> : page_shared_kernel<HD, 2, false>)
-                          : (plan.stream ? page_shared_kernel<HD, 1, true> : page_shared_kernel<HD, 1, false>);
+  const auto kernel = plan.row_blocks == 1    ? (plan.stream ? page_shared_kernel<HD, 1, 2, true> : page_shared_kernel<HD, 1, 2, false>)
+                      : plan.prefix_terms == 2 ? (plan.stream ? page_shared_kernel<HD, 2, 2, true> : page_shared_kernel<HD, 2, 2, false>)
+                                               : (plan.stream ? page_shared_kernel<HD, 2, 1, true> : page_shared_kernel<HD, 2, 1, false>);
   hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -261,11 +261,11 @@ hipError_t launch_decode_bf16(const AttnShape& s, const bf16_t* q, const bf16_t*
                               bool interleaved, hipStream_t stream);
 
 // Attention of n_new new tokens per request over pages (see PageAttnArgs: base_len, n_valid, max_base, offset), where
-// groups of requests share a prefix.  bf16.  The plan: `row_blocks` blocks of 64 query rows per workgroup, key ranges of
-// a group's prefix and of a request's own slots, each with that many tiles of query rows.
+// groups of requests share a prefix.  bf16.  The plan: `row_blocks` blocks of 64 query rows per workgroup and terms of a
+// probability over a prefix, key ranges of a group's prefix and of a request's own slots, each with that many tiles of query rows.
 constexpr int kSharedMaxSplits = 64;   // key ranges of a prefix, and of a request's own slots
 struct SharedPlan {
-  int32_t row_blocks = 1, prefix_splits = 1, own_splits = 1, prefix_row_tiles = 0, own_row_tiles = 0;
+  int32_t row_blocks = 1, prefix_terms = 2, prefix_splits = 1, own_splits = 1, prefix_row_tiles = 0, own_row_tiles = 0;
   int64_t prefix_blocks = 0, own_blocks = 0;   // workgroups per layer
   size_t ws_bytes = 0;
   bool stream = false;   // rows are read once and past the last-level cache
