@@ -227,6 +227,9 @@ __device__ __forceinline__ void part_of(const PageSharedArgs& a, int block, cons
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qv[nb][ks] = r < n_rows ? qp[4 * ks + g4] : u32x4{0, 0, 0, 0};
     row_ok[nb] = r < n_rows && lim[nb] >= 0;
+    // (rows of padding hold anything: they are asked for with the others, and are no queries)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qv[nb][ks] = row_ok[nb] ? qv[nb][ks] : u32x4{0, 0, 0, 0};
   }
   // (uniform) keys before `clear` are seen by every row of the workgroup
   int clear = INT32_MAX;
@@ -332,10 +335,12 @@ __device__ __forceinline__ void part_of(const PageSharedArgs& a, int block, cons
       m_tile[nb] = column_max(mx) * a.scale_log2;
       rises |= m_tile[nb] > m_run[nb] + 8.f;
     }
-    if (__any(rises)) {   // lazy reference max: p <= 2^8 (so values up to 2^120 over the number of keys)
+    // lazy reference max: p <= 2^8 (so values up to 2^120 over the number of keys).  Each column's own scores alone raise its
+    // maximum: the columns of a wave are different requests', and a row's rounding is not to depend on its neighbours.
+    if (__any(rises)) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const float m_new = fmaxf(m_run[nb], m_tile[nb]);
+        const float m_new = m_tile[nb] > m_run[nb] + 8.f ? m_tile[nb] : m_run[nb];
         const float alpha = __builtin_amdgcn_exp2f(m_run[nb] - m_new);
         m_run[nb] = m_new;
         l_part[nb] *= alpha;
