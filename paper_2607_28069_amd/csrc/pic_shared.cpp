@@ -102,7 +102,7 @@ SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, in
   const int64_t grouped = (int64_t)m.n_groups * m.max_group;
   int64_t most = 0;
   if (prefix_tiles > 0 && grouped > 0)
-    most = std::max(rows, std::min({65536 * ceil_of(s.batch, grouped), 512 * s.batch * own_rows, rows * std::min<int64_t>(prefix_tiles, kSharedMaxSplits)}));
+    most = std::max(rows, std::min({65536 * ceil_of(s.batch, grouped), (int64_t)512 * s.batch * own_rows, rows * std::min<int64_t>(prefix_tiles, kSharedMaxSplits)}));
   const int64_t all_tiles = ceil_of((int64_t)max_ctx + n_new, kSharedKeys);
   most += std::max(rows, std::min(512 * std::min<int64_t>(64, own_rows), rows * std::min<int64_t>((all_tiles + 1) / 2, kSharedMaxSplits)));
   p.ws_bytes = (size_t)most * (s.head_dim + 2) * sizeof(float);
