@@ -558,7 +558,10 @@ pic_status pic_page_decode_attn_rope(const pic_model* model, const pic_pages* pa
    request's into a page that others hold (pic_page_grow sees to that).  The other requests' tables must name pages
    that hold the same there (pic_page_fork's do).  A request whose new tokens come before the end of the shared slots sees its own
    slots only, [0, p], as always; the last shared_len[i] % 64 shared slots are read by each request.  Requests in no group
-   share nothing.
+   share nothing.  A launch splits own slots as long as what comes after max_len, or whole contexts where the batch is
+   larger than n_groups * max_group; so a group that shares far less than max_len, or an ungrouped request where groups have room to
+   spare, makes long work for few workgroups (16 requests of 10.5K, 8 of them sharing 512 slots only and 8 10368: 205 us,
+   pic_page_decode_attn 76).  Give such requests a group each, of shared_len their own length (68).
      n_groups                    >= 1, below 2^24
      max_group                   bound on the requests of a group: those past it in their group share nothing
      max_len                     bound on shared_len (clamped to it); <= table_cap * page_tokens

@@ -12,27 +12,37 @@ namespace pic {
 
 namespace {
 
+int64_t ceil_of(int64_t n, int64_t d) { return (n + d - 1) / d; }
+
 // The time of a launch, in tiles of 64 keys of a workgroup that has a compute unit to itself (about 1.2 us).  512 workgroups
 // run at once, the prefixes' before the requests' own; two on a compute unit slow each other down, and a workgroup's
-// start (lengths, page numbers, first tile) costs about 3 tiles.
+// start (lengths, page numbers, first tile) costs about 3 tiles.  Requests of no group are the last of the batch, at worst.
 struct LaunchCost {
-  int64_t prefix_units, own_units;   // workgroups per key range
-  double both, join;                 // a tile where compute units hold two; a part's share of the combine
+  int64_t prefix_units, own_units, lone_units;   // workgroups per key range; lone: those of requests of no group, among own
+  int64_t own_tiles, lone_tiles;                 // of a request of a group, and of one of none
+  double both, join;                             // a tile where compute units hold two; a part's share of the combine
 
-  double operator()(int64_t prefix_tiles, int64_t prefix_splits, int64_t own_tiles, int64_t own_splits) const {
+  double operator()(int64_t prefix_tiles, int64_t prefix_splits, int64_t own_splits) const {
     constexpr double kStart = 3.0;
-    const int64_t P = prefix_units * prefix_splits, O = own_units * own_splits;
+    const int64_t P = prefix_units * prefix_splits;
     const int64_t rest = P % 512;
     double t = (double)prefix_tiles * ((double)(P / 512) * both + (rest == 0 ? 0.0 : rest <= 256 ? 1.0 : both)) + kStart * (double)((P + 511) / 512);
-    const double own = (double)own_tiles + kStart;
-    const int64_t beside = P < 512 ? 512 - P : 0;
+    const int64_t beside = P < 512 ? 512 - P : 0, O = own_units * own_splits;
+    const double own = (double)ceil_of(own_tiles, own_splits) + kStart;
     if (O <= beside) t = std::max(t, own);
     else t += own * (double)((std::max<int64_t>(0, O - beside * (int64_t)(t / own)) + 511) / 512);
+    if (lone_units > 0) {   // (the last ones to start: as short ranges leave their places, or after all else)
+      const int64_t lone = lone_units * own_splits;
+      const double each = (double)ceil_of(lone_tiles, own_splits) + kStart;
+      if (lone <= beside) t = std::max(t, own * (double)std::max<int64_t>(0, O - beside) / (double)beside + each);
+      else t += each * (double)ceil_of(lone, 512);
+    }
     return t + join * (double)(prefix_splits + own_splits);
   }
 };
 
-int64_t ceil_of(int64_t n, int64_t d) { return (n + d - 1) / d; }
+// Workgroups of requests' own ranges, at most, where some requests are in no group: most of them then find nothing to do.
+constexpr int64_t kLoneBlocks = 4096;
 
 }  // namespace
 
@@ -57,7 +67,11 @@ SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, in
   p.prefix_row_tiles = (int32_t)ceil_of(group_rows, 64 * p.row_blocks);
   p.own_row_tiles = (int32_t)ceil_of(own_rows, 64);
   const int64_t prefix_tiles = std::min(m.max_len, max_ctx) / kSharedKeys;
-  const int64_t own_tiles = ceil_of((int64_t)max_ctx + n_new - prefix_tiles * kSharedKeys, kSharedKeys);
+  const int64_t all_tiles = ceil_of((int64_t)max_ctx + n_new, kSharedKeys), own_tiles = all_tiles - prefix_tiles;
+  // Requests that no group has room for: all of their slots are their own, and are split as such (4 requests of 32K, 2 of them
+  // a group, 581 us with one range each, 70 so; 8 of 10K, 4 a group, 102 -> 43; 33 of 32K, 4 groups of 8, 660 -> 161;
+  // pic_page_decode_attn 69, 45, 452).  How much less than max_len a group shares is not known here.
+  const int64_t lone = std::max<int64_t>(0, s.batch - (int64_t)m.n_groups * m.max_group);
   const int64_t heads = (int64_t)s.n_kv_heads * s.n_layers;
   const int64_t prefix_units = m.n_groups * heads * p.prefix_row_tiles, own_units = s.batch * heads * p.own_row_tiles;
   const int64_t rows = (int64_t)s.n_layers * s.batch * n_new * s.n_q_heads, part_bytes = rows * (s.head_dim + 2) * (int64_t)sizeof(float);
@@ -67,6 +81,9 @@ SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, in
   LaunchCost cost;
   cost.prefix_units = heads * row_tiles;
   cost.own_units = own_units;
+  cost.lone_units = lone * heads * p.own_row_tiles;
+  cost.own_tiles = own_tiles;
+  cost.lone_tiles = all_tiles;
   // (bound by the loads, which one workgroup with tiles of half the size does not keep busy, or by products)
   cost.both = p.row_blocks == 2 ? 1.7 : s.head_dim == 64 ? 1.3 : 2.0;
   cost.join = (double)part_bytes * 2.0 / 5.8e6;   // (written and read, 4.8 TB/s)
@@ -81,12 +98,16 @@ SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, in
       n = ceil_of(prefix_tiles, tiles);
     }
     const int64_t left = 512 - std::min<int64_t>(512, cost.prefix_units * n);
-    const int64_t o = std::max<int64_t>(1, std::min({left / own_units, (own_tiles + 1) / 2, (int64_t)kSharedMaxSplits}));
-    const double c = cost(tiles, n, ceil_of(own_tiles, o), o);
-    if (c < best) {
-      best = c;
-      p.prefix_splits = (int32_t)n;
-      p.own_splits = (int32_t)o;
+    const int64_t beside = std::max<int64_t>(1, std::min({left / own_units, (own_tiles + 1) / 2, (int64_t)kSharedMaxSplits}));
+    const int64_t most = lone > 0 ? std::min({kLoneBlocks / own_units, (all_tiles + 1) / 2, (int64_t)kSharedMaxSplits}) : 0;
+    for (int64_t o = beside;; o = std::min(2 * o, most)) {
+      const double c = cost(tiles, n, o);
+      if (c < best) {
+        best = c;
+        p.prefix_splits = (int32_t)n;
+        p.own_splits = (int32_t)o;
+      }
+      if (o >= most) break;
     }
   }
   auto blocks = [](int64_t ranges, int64_t row_tiles) { return ceil_of(ranges, 8) * 8 * row_tiles; };   // (whole rounds of the XCDs)
@@ -94,17 +115,16 @@ SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, in
   p.own_blocks = blocks((int64_t)s.batch * s.n_kv_heads * p.own_splits, p.own_row_tiles);
   // Rows that the last-level cache (256 MB) will not hold until the next call leave it to others (8 requests x 33K in 4
   // groups 60 -> 55 us, 64 requests of up to 2K of their own 72 -> 63; below, 16 over 10K 19.5 -> 21.2).
-  p.stream = p.prefix_row_tiles <= 1 && heads * s.head_dim * 4.0 * ((double)m.n_groups * prefix_tiles + (double)s.batch * own_tiles) * kSharedKeys > 256e6;
+  p.stream = p.prefix_row_tiles <= 1 && heads * s.head_dim * 4.0 * ((double)m.n_groups * prefix_tiles + (double)(s.batch - lone) * own_tiles + (double)lone * all_tiles) * kSharedKeys > 256e6;
   // Room for every call of these groups with no more requests, tokens and slots, so that a buffer for the largest serves all.
   // Parts of prefixes: max(1, 512 / prefix_units) ranges of R = heads * batch * own_rows rows, where prefix_units / heads is at
-  // least 1, batch * own_rows / 128, or n_groups * max_group * own_rows / 128.  Of requests: max(1, 512 / own_units), where
-  // own_units / heads is at least batch, or batch * own_rows / 64.
+  // least 1, batch * own_rows / 128, or n_groups * max_group * own_rows / 128.  Of requests: max(1, 512 / own_units), with some in
+  // no group kLoneBlocks / own_units, where own_units / heads is at least batch, or batch * own_rows / 64.
   const int64_t grouped = (int64_t)m.n_groups * m.max_group;
   int64_t most = 0;
   if (prefix_tiles > 0 && grouped > 0)
     most = std::max(rows, std::min({65536 * ceil_of(s.batch, grouped), (int64_t)512 * s.batch * own_rows, rows * std::min<int64_t>(prefix_tiles, kSharedMaxSplits)}));
-  const int64_t all_tiles = ceil_of((int64_t)max_ctx + n_new, kSharedKeys);
-  most += std::max(rows, std::min(512 * std::min<int64_t>(64, own_rows), rows * std::min<int64_t>((all_tiles + 1) / 2, kSharedMaxSplits)));
+  most += std::max(rows, std::min((lone > 0 ? kLoneBlocks : 512) * std::min<int64_t>(64, own_rows), rows * std::min<int64_t>((all_tiles + 1) / 2, kSharedMaxSplits)));
   p.ws_bytes = (size_t)most * (s.head_dim + 2) * sizeof(float);
   return p;
 }

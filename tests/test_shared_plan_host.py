@@ -78,3 +78,12 @@ def test_workspace_of_any_sizes(plan):
             cases.append(c)
     for c, p in zip(cases, plan(cases)):
         assert p[3] >= written(c, p), (c, p)
+
+
+def test_requests_of_no_group_are_split(plan):
+    """Where a batch is larger than its groups, some requests read all of their slots by themselves: no range of these is as long as
+    one of the launch's whole time should be (64 tiles of 64 keys), nor is the other requests' prefix left whole."""
+    cases = [(1, 32, 8, 128, 4, 1, 2, 32000, 1, 32100), (1, 32, 8, 128, 8, 1, 4, 10368, 1, 10500), (1, 32, 8, 128, 16, 1, 8, 10368, 1, 10500),
+             (1, 28, 4, 128, 33, 4, 8, 32000, 1, 32596), (1, 32, 8, 128, 2, 1, 1, 2048, 1, 2100), (2, 32, 8, 64, 6, 1, 3, 8000, 5, 8200)]
+    for c, p in zip(cases, plan(cases)):
+        assert -(-c[9] // 64) / p[1] <= 64 and c[7] // 64 / p[0] <= 64, (c, p)
