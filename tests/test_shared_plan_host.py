@@ -87,3 +87,10 @@ def test_requests_of_no_group_are_split(plan):
              (1, 28, 4, 128, 33, 4, 8, 32000, 1, 32596), (1, 32, 8, 128, 2, 1, 1, 2048, 1, 2100), (2, 32, 8, 64, 6, 1, 3, 8000, 5, 8200)]
     for c, p in zip(cases, plan(cases)):
         assert -(-c[9] // 64) / p[1] <= 64 and c[7] // 64 / p[0] <= 64, (c, p)
+
+
+def test_parts_of_many_rows(plan):
+    """Rows so many that each part costs more than the prefix are given few: most of 4096 requests share nothing here."""
+    cases = [(1, 8, 1, 128, 4096, 1, 2, 2048, n, 2100) for n in (1, 8)] + [(1, 8, 1, 128, 4096, 3, 700, 2048, 8, 2100)]
+    for c, p in zip(cases, plan(cases)):
+        assert p[0] <= 16, (c, p)
