@@ -677,6 +677,8 @@ def _token_rows(t, heads, head_dim, name, at):
         elif strides[i] != span:
             raise ValueError(f"{name}: tokens must lie one step apart")
         span = shape[i] * strides[i]
+    if span == 0 and t.numel() > 0:   # (a step of 0 stands for dense rows in the call)
+        raise ValueError(f"{name}: tokens must lie one step apart, not at one place")
     if t.get_device() != at:   # (-1 for a host tensor)
         raise ValueError("device buffer expected: got a host tensor" if not t.is_cuda else
                          f"{name} on device {t.get_device()}, the current one is {at}")
