@@ -97,14 +97,21 @@ class QkNorm(ctypes.Structure):
     head that turns.  Holds on to the weights."""
     _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
                 ("rope_dim", ctypes.c_int32), ("rope_order", ctypes.c_int32), ("rope_scale", ctypes.c_float)]
+    weights = n_weights = device = None   # (of the tensors: fewest elements, where they are)
 
     @classmethod
     def of(cls, q_weight, k_weight, eps=1e-6, rope_dim=0, rope_order="keep", rope_scale=1.0):
         order = {"keep": PIC_ROPE_ORDER_KEEP, "pairs": PIC_ROPE_ORDER_PAIRS}.get(rope_order, rope_order)
+        x = cls(None, None, float(eps), int(rope_dim), order, float(rope_scale))
         for w in (q_weight, k_weight):
-            if w is not None and str(w.dtype) != "torch.float32":
+            if w is None:
+                continue
+            if str(w.dtype) != "torch.float32":
                 raise ValueError("weights: float32 expected")
-        x = cls(_ptr(q_weight), _ptr(k_weight), float(eps), int(rope_dim), order, float(rope_scale))
+            if x.device not in (None, w.get_device()):
+                raise ValueError("weights: on two devices")
+            x.n_weights, x.device = min(w.numel(), x.n_weights or w.numel()), w.get_device()
+        x.q_weight, x.k_weight = _ptr(q_weight), _ptr(k_weight)
         x.weights = (q_weight, k_weight)
         return x
 
@@ -605,6 +612,7 @@ def pic_page_shared_suffix_attn(model: Model, pages: Pages, shared: Shared, q, k
                                 scale=0.0, stream=None):
     """group_start: device int32 [n_groups + 1], or None (one group); shared_len: device int32 [n_groups]."""
     _device_i32((group_start, shared.n_groups + 1, "group_start"), (shared_len, shared.n_groups, "shared_len"))
+    _at_least_i32((page_table, batch * pages.table_cap, "page_table"), (ctx_len, batch, "ctx_len"), (n_valid, batch, "n_valid"))
     (*a, tab, gs, sl, lens, nv, o, ws), st = _on_device((q, k_suf, v_suf, pages_k, pages_v, page_table, group_start, shared_len,
                                                          ctx_len, n_valid, out, workspace), stream)
     _check(load().pic_page_shared_suffix_attn(ctypes.byref(model), ctypes.byref(pages), ctypes.byref(shared), *a, tab, int(batch),
@@ -617,6 +625,7 @@ def pic_page_shared_decode_attn(model: Model, pages: Pages, shared: Shared, q, k
                                 stream=None):
     """group_start: device int32 [n_groups + 1], or None (one group); shared_len: device int32 [n_groups]."""
     _device_i32((group_start, shared.n_groups + 1, "group_start"), (shared_len, shared.n_groups, "shared_len"))
+    _at_least_i32((page_table, batch * pages.table_cap, "page_table"), (base_len, batch, "base_len"))
     (*a, tab, gs, sl, lens, o, ws), st = _on_device((q, k_new, v_new, pages_k, pages_v, page_table, group_start, shared_len,
                                                      base_len, out, workspace), stream)
     _check(load().pic_page_shared_decode_attn(ctypes.byref(model), ctypes.byref(pages), ctypes.byref(shared), *a, tab, int(batch),
@@ -635,6 +644,15 @@ def _device_i32(*sizes):
     for t, n, name in sizes:
         if t is not None and (t.dtype is not i32 or t.numel() != n):
             raise ValueError(f"{name}: {n} int32 entries expected, got {t.numel()} of {t.dtype}")
+
+
+def _at_least_i32(*sizes):
+    """As _device_i32, for buffers that may be of a larger batch."""
+    import torch
+    i32 = torch.int32
+    for t, n, name in sizes:
+        if t is not None and (t.dtype is not i32 or t.numel() < n):
+            raise ValueError(f"{name}: at least {n} int32 entries expected, got {t.numel()} of {t.dtype}")
 
 
 def pic_page_grow_async(pages: Pages, batch, refs, page_table, base_len, n_new, pairs, ready, result, workspace, n_valid=None,
@@ -691,7 +709,21 @@ def pic_qk_norm_rope(model: Model, how: QkNorm, q, k, v, batch, n_new, table, ma
     v_out: heads normalised and turned to positions base_len[b] + offset + i."""
     hq, hkv, d = model.n_q_heads, model.n_kv_heads, model.head_dim
     import torch
+    dtype, rows = torch.float32 if model.dtype == PIC_F32 else torch.bfloat16, model.n_layers * batch * n_new * d
+    for name, t, out, heads in (("q", q, q_out, hq), ("k", k, k_out, hkv), ("v", v, v_out, hkv)):
+        if t is None:
+            continue
+        for x in (t, out):
+            if x is not None and (x.dtype is not dtype or x.numel() < rows * heads):
+                raise ValueError(f"{name}: at least {rows * heads} elements of {dtype} expected, got {x.numel()} of {x.dtype}")
+    _at_least_i32((base_len, batch, "base_len"), (n_valid, batch, "n_valid"))
+    if how.n_weights is not None and how.n_weights < model.n_layers * d:
+        raise ValueError(f"weights: {model.n_layers * d} float32 expected, got {how.n_weights}")
+    if table is not None and _ws_bytes(table) < 4 * d * (max_abs_delta + 1) * max(model.rope_tables, 1):
+        raise ValueError(f"table: {_ws_bytes(table)} bytes, fewer than max_abs_delta {max_abs_delta} takes")
     at = torch.cuda.current_device()
+    if how.device is not None and how.device != at:
+        raise ValueError(f"weights on device {how.device}, the current one is {at}")
     (lens, nv, tab, qo, ko, vo), st = _on_device((base_len, n_valid, table, q_out, k_out, v_out), stream)
     _check(load().pic_qk_norm_rope(ctypes.byref(model), ctypes.byref(how), *_token_rows(q, hq, d, "q", at),
                                    *_token_rows(k, hkv, d, "k", at), *_token_rows(v, hkv, d, "v", at), int(batch), lens,
