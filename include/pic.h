@@ -560,10 +560,11 @@ pic_status pic_page_decode_attn_rope(const pic_model* model, const pic_pages* pa
    slots only, [0, p], as always; the last shared_len[i] % 64 shared slots are read by each request.  Requests in no group
    share nothing.  A launch splits own slots as long as what comes after max_len, or whole contexts where the batch is
    larger than n_groups * max_group; so a group that shares far less than max_len, or an ungrouped request where groups have room to
-   spare, makes long work for few workgroups (16 requests of 10.5K, 8 of them sharing 512 slots only and 8 10368: 205 us,
+   spare, makes long work for few workgroups (16 requests of 10.5K, 8 of them sharing 512 slots only and 8 10368: 205 to 220 us,
    pic_page_decode_attn 76).  Give such requests a group each, of shared_len their own length (68).
      n_groups                    >= 1, below 2^24
-     max_group                   bound on the requests of a group: those past it in their group share nothing
+     max_group                   bound on the requests of a group: those past it in their group share nothing.  It sets the query
+                                 rows that a launch plans for: one far above the groups costs time (32 of two, 64: 120 us, 2: 98)
      max_len                     bound on shared_len (clamped to it); <= table_cap * page_tokens
      group_start [device, n_groups + 1]  increasing; NULL: one group, the whole batch (n_groups 1)
      shared_len  [device, n_groups]
@@ -571,10 +572,10 @@ pic_status pic_page_decode_attn_rope(const pic_model* model, const pic_pages* pa
                                  these or larger max_len, batch, n_new (decode: 1) and max_ctx (decode: max_base_len + step)
    (the other arguments, padding, what is stored and what is not finite as for pic_page_suffix_attn and
    pic_page_decode_attn; queries and keys rotated; n_suffix * Hkv below 2^24.)  Probabilities keep
-   16 bits; but over shared slots 8 where a request has more than 32 query rows per kv head (n_suffix * Hq / Hkv) and a group,
-   of max_group requests, more than 64.  Last bits depend on the batch and on the bounds, which set the key ranges of the launch, never on the lengths of other
-   requests.  On float32 pages the calls are those two, request by
-   request, and need no workspace. */
+   16 bits, but 8 over shared slots where a request has more than 32 query rows per kv head (n_suffix * Hq / Hkv) and a group,
+   of max_group requests, more than 64 (pic_page_suffix_attn's 8).  Last bits depend on the batch's size and on the bounds, which
+   set the key ranges of the launch, and on what the request and its group's shared slots hold, never on the other requests.  On
+   float32 pages the calls are those two, request by request, at their times, and need no workspace. */
 typedef struct {
   int32_t n_groups;
   int32_t max_group;

@@ -14,9 +14,9 @@
 //    to its limit; tiles that some row of the workgroup sees in part are masked, and values there that are not finite
 //    cleared in LDS, so that rows that do not see them stay as they are (the others get them back at the end).
 //
-// Measured (combine included, 32 + 2 x 8 heads of 128): 2 requests over 2K 10 us, 16 over 10K 19.6, 64 over 16K 42, each about 1.2
-// us a tile of 64 keys that a workgroup has to itself, the first one after 4 to 5 where all start at once; 37 requests in
-// 4 groups of up to 32K (28 + 2 x 4 heads) 51 us, 4.3 TB/s in all; 16 x 24 tokens over 10K 79 us, 820 TFLOP/s.
+// Measured (combine included, 32 + 2 x 8 heads of 128): 2 requests over 2K 11 us, 16 over 10K 19, 64 over 16K 49, about 1.2 us a
+// tile of 64 keys that a workgroup of 64 rows has to itself, the first one after 4 to 5 where all start at once; 37 requests in
+// 4 groups of up to 32K (28 + 2 x 4 heads) 57 us, 3.9 TB/s in all; 16 x 24 tokens over 10K 80 us, 820 TFLOP/s.
 #include <type_traits>
 
 #include "decode_common.h"
@@ -549,7 +549,7 @@ hipError_t launch_hd(const PageSharedArgs& a, const SharedPlan& plan, dim3 grid,
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // Few parts, or more rows than workgroups fit the GPU at once (2 layers of 12 x 5 tokens, 32 heads of 64, 9 parts: 27.2 -> 25
-  // us for the call; 224 rows of 16 parts 8.9 -> 9.3): lanes a row.  Else the combine of page_decode.hip, a workgroup a row
+  // us for the call, 31.0 -> 29.0 with two terms; 224 rows of 16 parts 8.9 -> 9.3): lanes a row.  Else the combine of page_decode.hip, a workgroup a row
   // (512 rows of 28 parts 19.8 us, 21.0 the other way).
   const int parts = a.prefix_splits + a.own_splits;
   const int64_t row_count = (int64_t)s.n_layers * s.batch * a.n_new * s.n_q_heads;

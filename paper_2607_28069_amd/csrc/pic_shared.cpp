@@ -49,10 +49,11 @@ constexpr int64_t kLoneBlocks = 4096;
 // Key ranges of a launch: as many as cover some or all compute units, or up to twice, whichever the estimate above puts first
 // (few where a prefix is short and its rows many, as each range writes a part of every row, which the combine reads), requests'
 // own ranges filling what is left.  Measured, us by ranges of the prefix (head_dim 128, 8 kv heads):
-// 64 requests over 16K + 300 own (16 workgroups a range) 16: 41.5, 24: 47, 32: 49; 16 over 10K (8) 20: 21.3, 28: 19.0, 40:
-// 22.1; 16 x 24 tokens over 10K (96) 2: 143, 4: 92, 5: 86, 8: 107; 4 groups of up to 32K (16) 16: 63, 24: 60, 28: 55 (at
-// head_dim 64, or with 64 rows at most, such a share of the second place on every compute unit loses 1 to 2 us); 32 over 2K
-// (8) 31: 20.2, 16: 17.8; 4 x 4 tokens over 2K (8) 31: 15.3, 16: 12.8; 16 over 2K (8) 31: 14.5, 16: 12.7.
+// 64 requests over 16K + 300 own (16 workgroups a range) 12: 54.6, 16: 47.8, 24: 52.3, 32: 58.1; 16 over 10K (8) 20: 21.3, 28:
+// 19.1, 40: 22.0; 16 x 24 tokens over 10K (96) 2: 143, 4: 92, 5: 86, 8: 107; 4 groups of up to 32K (16) 16: 68, 24: 62, 28: 57,
+// 32: 63 (at head_dim 64, or with 64 rows at most, such a share of the second place on every compute unit loses 1 to 2 us); 12 x 5
+// tokens at head_dim 64 (48) 5: 35, 8: 29, 11: 33; 32 over 2K (8) 31: 17.9, 16: 18.0, 8: 19.8; 4 x 4 tokens over 2K (8) 31: 15.3, 16:
+// 12.8; 16 over 2K (8) 31: 14.5, 16: 12.7.
 SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, int32_t max_ctx) {
   SharedPlan p;
   const int64_t n_rep = s.n_q_heads / s.n_kv_heads;
@@ -124,7 +125,8 @@ SharedPlan plan_shared(const AttnShape& s, const SharedMap& m, int32_t n_new, in
   p.own_blocks = blocks((int64_t)s.batch * s.n_kv_heads * p.own_splits, p.own_row_tiles);
   // Rows that the last-level cache (256 MB) will not hold until the next call leave it to others (8 requests x 33K in 4
   // groups 60 -> 55 us, 64 requests of up to 2K of their own 72 -> 63; below, 16 over 10K 19.5 -> 21.2).
-  p.stream = p.prefix_row_tiles <= 1 && heads * s.head_dim * 4.0 * ((double)m.n_groups * prefix_tiles + (double)(s.batch - lone) * own_tiles + (double)lone * all_tiles) * kSharedKeys > 256e6;
+  const double tiles_read = (double)m.n_groups * prefix_tiles + (double)(s.batch - lone) * own_tiles + (double)lone * all_tiles;
+  p.stream = p.prefix_row_tiles <= 1 && heads * s.head_dim * 4.0 * tiles_read * kSharedKeys > 256e6;
   // Room for every call of these groups with no more requests, tokens and slots, so that a buffer for the largest serves all.
   // Parts of prefixes: max(1, 512 / prefix_units) ranges of R = heads * batch * own_rows rows, where prefix_units / heads is at
   // least 1, batch * own_rows / 128, or n_groups * max_group * own_rows / 128.  Of requests: max(1, 512 / own_units), with some in
@@ -202,7 +204,9 @@ pic_status shared_attn(const pic_model* model, const pic_pages* pages, const pic
   if (!base_len) return fail(PIC_ERR_INVALID_ARG, decode ? "base_len is NULL" : "ctx_len is NULL");
   if (!shared_len) return fail(PIC_ERR_INVALID_ARG, "shared_len is NULL");
   if (!group_start && shared->n_groups != 1) return fail(PIC_ERR_INVALID_ARG, "group_start is NULL, and there are %d groups", shared->n_groups);
-  if (model->dtype == PIC_F32) {   // (bound by the float32 matrix rate, whatever is read)
+  // Request by request: a long suffix is bound by the float32 matrix rate, whatever is read.  (A decode is not: 16 requests over 10K
+  // take 210 us, where the shared bytes and the products are 18 each.)
+  if (model->dtype == PIC_F32) {
     return decode ? pic_page_decode_attn(model, pages, q, k_new, v_new, pages_k, pages_v, page_table, batch, base_len, offset, max_base,
                                          scale, 0, out, workspace, ws_bytes, stream)
                   : pic_page_suffix_attn(model, pages, q, k_new, v_new, pages_k, pages_v, page_table, batch, base_len, max_base,
