@@ -110,7 +110,7 @@ class QkNorm(ctypes.Structure):
                 raise ValueError("weights: float32 expected")
             if x.device not in (None, w.get_device()):
                 raise ValueError("weights: on two devices")
-            x.n_weights, x.device = min(w.numel(), x.n_weights or w.numel()), w.get_device()
+            x.n_weights, x.device = w.numel() if x.n_weights is None else min(w.numel(), x.n_weights), w.get_device()
         x.q_weight, x.k_weight = _ptr(q_weight), _ptr(k_weight)
         x.weights = (q_weight, k_weight)
         return x
